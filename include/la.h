@@ -70,7 +70,8 @@ typedef enum {
     LA_ERR_RUNTIME = 3,
     LA_ERR_WORKSPACE = 4
 } la_status;
-typedef enum { LA_F32 = 0, LA_F64 = 1 } la_dtype;
+/* LA_BF16 and LA_F16: for the sequence-layer operators (la_delta_rule and below it) only */
+typedef enum { LA_F32 = 0, LA_F64 = 1, LA_BF16 = 2, LA_F16 = 3 } la_dtype;
 typedef enum {
     LA_OP_POTRF = 0,
     LA_OP_POTRF_BACKWARD = 1,
@@ -327,6 +328,80 @@ la_status la_sgp_criterion(la_dtype dt, int U, int n, const void *Kuu, const voi
 la_status la_kalman_filter(la_dtype dt, int64_t batch, int T, int dh, int dv, int shared_params, const void *A,
                            const void *B, const void *Sh, const void *Sv, const void *mu0, const void *S0,
                            const void *v, void *f, void *F, void *nll, int32_t *info, void *stream);
+
+/* ---------------------------------------------------------------------------------
+ * A recurrent sequence layer and its training step: the gated delta rule, layer norm, the norm of
+ * all gradients.  The conventions above hold; in addition dt may be LA_BF16 or LA_F16 (sums,
+ * statistics, states and norms are held in 32 bits or more, results rounded once).
+ * ---------------------------------------------------------------------------------
+ *
+ * Gated delta rule.  Per sequence and value head, with a state S [dk, dv] of float, S_0 the initial one,
+ *   S_t = a_t S_{t-1} + k_t u_t^T,   a_t = exp(g_t),   u_t = beta_t (v_t - a_t S_{t-1}^T k_t),
+ *   o_t = scale S_t^T q_t.
+ * dt is LA_F32, LA_BF16 or LA_F16 (LA_F64: LA_ERR_UNSUPPORTED), the type of q, k, v, o and their gradients;
+ * g, beta, the states and their gradients are float.  1 <= dk <= 128, 1 <= dv <= 1024 (above: LA_ERR_UNSUPPORTED).
+ * Value head h reads key head h / (hv / hk); hk divides hv.
+ *   q, k [tokens of all sequences, hk, dk], v [.., hv, dv]: ldq, ldk, ldv elements from a token to the
+ *   next (views of a wider projection); g, beta [.., hv], o [.., hv, dv] dense.
+ *   offsets NULL: `batch` sequences of `tokens` tokens each.  Else int32 [batch + 1], ascending: sequence n is
+ *   tokens offsets[n] .. offsets[n + 1] - 1 of the `tokens` there are in all, none of them as well; o of tokens before the first
+ *   offset or from the last one on is zero.  (The offsets are read on the GPU and kept inside 0 .. tokens.)
+ *   initial_state [batch, hv, dk, dv] or NULL (zeros); state: the final states, same shape, or NULL; it may be
+ *   the same buffer as initial_state.  No other operands overlap.
+ * g is meant to be <= 0; one below -1000 counts as -1000, which clears the state.  With beta |k|^2 above 2 the recurrence itself
+ * grows.  A NaN or an infinity reaches, besides what follows it in its sequence, at most the tokens of its own chunk (64 in bf16, else 32) before it.
+ * workspace: la_delta_rule_workspace_bytes(.., packed = offsets != NULL).  saved: NULL, or 256-byte aligned device memory of
+ * la_delta_rule_saved_bytes that la_delta_rule_backward then takes instead of running the forward pass again (no
+ * workspace is needed with it). */
+size_t la_delta_rule_workspace_bytes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, int packed);
+size_t la_delta_rule_saved_bytes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, int packed);
+la_status la_delta_rule(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, const int32_t *offsets,
+                        const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, const float *g,
+                        const float *beta, double scale, const float *initial_state, void *o, float *state, void *saved,
+                        size_t saved_bytes, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradient: from o_bar [.., hv, dv] (dense) and state_bar (the final states' gradient, or NULL) to q_bar, k_bar
+ * [.., hk, dk], v_bar [.., hv, dv], g_bar, beta_bar [.., hv] (all dense) and initial_state_bar (or NULL).  A key head's
+ * gradients are the sums over the value heads that read it, always in the same order.  saved: what la_delta_rule left for
+ * the same inputs, or NULL: the forward pass is run again.  Tokens of no sequence get zeros.  No operands overlap. */
+size_t la_delta_rule_backward_workspace_bytes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, int packed,
+                                              int with_saved);
+la_status la_delta_rule_backward(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, const int32_t *offsets,
+                                 const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, const float *g,
+                                 const float *beta, double scale, const float *initial_state, const void *o_bar,
+                                 const float *state_bar, const void *saved, size_t saved_bytes, void *q_bar, void *k_bar, void *v_bar,
+                                 float *g_bar, float *beta_bar, float *initial_state_bar, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/* One token of each of `batch` sequences, for serving: q, k [batch, hk, dk], v [batch, hv, dv] (ldq, ldk, ldv elements
+ * from a sequence to the next), g, beta [batch, hv], o [batch, hv, dv].  state [slots, hv, dk, dv]: a cache of states, updated
+ * in place; sequence n has state slot[n] (int32, device), or n where slot is NULL.  A slot outside 0 .. slots - 1 has no state:
+ * o is zero and nothing is updated.  The slots of one call are distinct.  No scratch memory. */
+la_status la_delta_rule_step(la_dtype dt, int64_t batch, int hk, int hv, int dk, int dv, const void *q, int64_t ldq, const void *k,
+                             int64_t ldk, const void *v, int64_t ldv, const float *g, const float *beta, double scale,
+                             float *state, int64_t slots, const int32_t *slot, void *o, void *stream);
+
+/* Layer norm of rows of n elements: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps).  x: row r starts
+ * at x + r ldx; y [rows, n] dense (it may be x where ldx == n).  weight, bias [n] of type wdt, or NULL (1 and 0): wdt is dt, or
+ * LA_F32 where dt is 16 bits wide.  mean, rstd [rows], both or neither: float, double for LA_F64; the gradient takes them. */
+la_status la_layer_norm(la_dtype dt, la_dtype wdt, int64_t rows, int n, int64_t ldx, const void *x, const void *weight, const void *bias,
+                        double eps, void *y, void *mean, void *rstd, void *stream);
+
+/* Its gradient: x_bar [rows, n] (it may be y_bar), weight_bar and bias_bar [n] of type wdt (either may be NULL).  The sums over rows
+ * are taken in an order that depends on the sizes alone.  y_bar is dense. */
+size_t la_layer_norm_backward_workspace_bytes(la_dtype dt, int64_t rows, int n);
+la_status la_layer_norm_backward(la_dtype dt, la_dtype wdt, int64_t rows, int n, int64_t ldx, const void *x, const void *y_bar,
+                                 const void *mean, const void *rstd, const void *weight, void *x_bar, void *weight_bar, void *bias_bar,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* The norm over all of `count` gradients, norm = sqrt(sum of their squares), and out = gradient * min(1, max_norm / norm).  types,
+ * sizes (elements), grads, out: HOST arrays, their pointers device memory; out[i] is grads[i] (in place) or does not overlap any
+ * gradient.  norm: one element of norm_type (LA_F32 or LA_F64), on the device.  Where the norm is not finite the gradients are
+ * passed on unchanged: the caller sees it in norm.  Squares are summed in 64 bits, in an order that depends on sizes and
+ * addresses' alignment alone.  max_norm >= 0, infinity as well (the norm alone). */
+size_t la_clip_gradients_workspace_bytes(int count, const int64_t *sizes);
+la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *sizes, const void *const *grads, void *const *out,
+                            double max_norm, la_dtype norm_type, void *norm, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Text of the last HIP error seen by this thread's calls (host pointer, never NULL). */
 const char *la_last_error(void);

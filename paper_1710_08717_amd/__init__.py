@@ -8,6 +8,12 @@ library is missing, importing the binding raises.
 """
 from .binding import (  # noqa: F401
     LaError,
+    clip_gradients,
+    delta_rule,
+    delta_rule_backward,
+    delta_rule_step,
+    layer_norm,
+    layer_norm_backward,
     potrf_noalloc,
     workspace_bytes,
     gemm2,
@@ -32,4 +38,5 @@ from .binding import (  # noqa: F401
 )
 
 __all__ = ["potrf", "potrf_backward", "trsm", "trmm", "syrk", "trsm_backward", "trmm_backward", "syrk_backward", "gemm2_backward", "potri", "potri_backward", "sgp_criterion", "kalman_filter", "gp_criterion", "sumlogdiag",
-           "gp_glue", "gemm2", "load", "lib_path", "LaError", "workspace_bytes", "potrf_noalloc"]
+           "gp_glue", "gemm2", "load", "lib_path", "LaError", "workspace_bytes", "potrf_noalloc",
+           "delta_rule", "delta_rule_backward", "delta_rule_step", "layer_norm", "layer_norm_backward", "clip_gradients"]

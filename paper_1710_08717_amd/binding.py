@@ -25,6 +25,9 @@ SYMBOLS = [
     "la_workspace_bytes", "la_potrf_batched_ws", "la_potrf_backward_ws", "la_trsm_batched_ws", "la_trmm_batched_ws",
     "la_syrk_batched_ws", "la_gemm2_batched_ws", "la_trsm_backward_ws", "la_trmm_backward_ws", "la_syrk_backward_ws",
     "la_gemm2_backward_ws", "la_potri_ws", "la_potri_backward_ws", "la_potrf_batched_noalloc",
+    "la_delta_rule_workspace_bytes", "la_delta_rule_saved_bytes", "la_delta_rule", "la_delta_rule_backward_workspace_bytes",
+    "la_delta_rule_backward", "la_delta_rule_step", "la_layer_norm", "la_layer_norm_backward_workspace_bytes", "la_layer_norm_backward",
+    "la_clip_gradients_workspace_bytes", "la_clip_gradients",
 ]
 
 # la_op of include/la.h
@@ -90,6 +93,22 @@ def load():
     lib.la_potrf_batched_noalloc.restype = i32
     lib.la_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32]
     lib.la_workspace_bytes.restype = ctypes.c_size_t
+    rule, sz = [i32, i64, i64, i32, i32, i32, i32], ctypes.c_size_t
+    rows = rule + [vp, vp, i64, vp, i64, vp, i64, vp, vp, f64, vp]  # offsets, q, k, v, g, beta, scale, initial_state
+    for name, args in (
+        ("la_delta_rule_workspace_bytes", rule + [i32]), ("la_delta_rule_saved_bytes", rule + [i32]),
+        ("la_delta_rule_backward_workspace_bytes", rule + [i32, i32]),
+        ("la_layer_norm_backward_workspace_bytes", [i32, i64, i32]), ("la_clip_gradients_workspace_bytes", [i32, vp]),
+        ("la_delta_rule", rows + [vp, vp, vp, sz, vp, sz, vp]),
+        ("la_delta_rule_backward", rows + [vp, vp, vp, sz] + [vp] * 6 + [vp, sz, vp]),
+        ("la_delta_rule_step", [i32, i64, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, f64, vp, i64, vp, vp, vp]),
+        ("la_layer_norm", [i32, i32, i64, i32, i64, vp, vp, vp, f64, vp, vp, vp, vp]),
+        ("la_layer_norm_backward", [i32, i32, i64, i32, i64] + [vp] * 8 + [vp, sz, vp]),
+        ("la_clip_gradients", [i32, vp, vp, vp, vp, f64, i32, vp, vp, sz, vp]),
+    ):
+        f = getattr(lib, name)
+        f.argtypes = args
+        f.restype = sz if name.endswith("_bytes") else i32
     # the _ws form of an entry point: its arguments with (workspace, workspace_bytes) before the stream
     for name in SYMBOLS:
         if name.endswith("_ws"):
@@ -509,3 +528,263 @@ def gp_glue(L, y, z, alpha, loss=None, Lbar=None):
         _check(load().la_gp_glue(_dt(L), _batch(L), n, _ptr(L), _ptr(y), _ptr(z), _ptr(alpha), _ptr(loss), _ptr(Lbar),
                                  _stream(L)), "la_gp_glue")
     return loss, Lbar
+
+
+# A recurrent sequence layer and its training step.  These take float32, bfloat16 and float16 (layer norm and clipping float64 as well); gates,
+# states, statistics and norms are float32 (float64 beside float64).
+_LAYER_TYPES = {torch.float32: 0, torch.float64: 1, torch.bfloat16: 2, torch.float16: 3}
+
+
+def _layer_dt(t):
+    if t.dtype not in _LAYER_TYPES:
+        raise LaError(f"unsupported dtype {t.dtype}")
+    return _LAYER_TYPES[t.dtype]
+
+
+def _on_gpu(device, dtype, **tensors):
+    """Each tensor that is not None: on `device`, of `dtype`, contiguous."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.device != device:
+            raise LaError(f"{name}: tensors must be on the same GPU")
+        if t.dtype != dtype:
+            raise LaError(f"{name}: {dtype} is wanted, got {t.dtype}")
+        if not t.is_contiguous():
+            raise LaError(f"{name}: tensors must be contiguous")
+
+
+def _shape(name, t, want):
+    if t is not None and tuple(t.shape) != tuple(want):
+        raise LaError(f"{name}: shape {tuple(want)} is wanted, got {tuple(t.shape)}")
+
+
+def _rows(name, t, inner):
+    """Elements from one row to the next of a tensor whose last `inner` axes are dense and whose leading axes are rows one distance apart."""
+    want = 1
+    if t.numel() == 0:
+        for i in range(t.dim() - inner, t.dim()):
+            want *= t.shape[i]
+        return want
+    for i in range(t.dim() - 1, t.dim() - 1 - inner, -1):
+        if t.shape[i] != 1 and t.stride(i) != want:
+            raise LaError(f"{name}: the last {inner} axes must be contiguous")
+        want *= t.shape[i]
+    ld, count = None, 1
+    for i in range(t.dim() - 1 - inner, -1, -1):
+        if t.shape[i] == 1:
+            continue
+        if ld is None:
+            ld = t.stride(i)
+            if ld < want:
+                raise LaError(f"{name}: rows must not overlap")
+        elif t.stride(i) != ld * count:
+            raise LaError(f"{name}: rows must be one distance apart")
+        count *= t.shape[i]
+    return want if ld is None else ld
+
+
+def _scratch(workspace, need, t):
+    """(tensor, pointer, bytes): the caller's uint8 device tensor, or a fresh one where the call needs some and none was given."""
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or workspace.device != t.device or not workspace.is_contiguous():
+            raise LaError("a workspace is a contiguous uint8 tensor on the same GPU")
+        return workspace, workspace.data_ptr(), workspace.numel()
+    if need == 0:
+        return None, 0, 0
+    buf = torch.empty(need, dtype=torch.uint8, device=t.device)
+    return buf, buf.data_ptr(), need  # the caller keeps buf until the call is enqueued
+
+
+class _Delta:
+    """Checked operands of the gated delta rule: q, k [batch, tokens, hk, dk], v [batch, tokens, hv, dv], g, beta [batch, tokens, hv]."""
+
+    def __init__(self, q, k, v, g, beta, offsets, lead=2):
+        if not q.is_cuda:
+            raise LaError("tensors must be on the GPU")
+        self.dt = _layer_dt(q)
+        if q.dtype == torch.float64:
+            raise LaError("the delta rule takes float32, bfloat16 and float16")
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            if t.dim() != lead + 2:
+                raise LaError(f"{name}: {lead + 2} axes are wanted, got {t.dim()}")
+            if t.dtype != q.dtype or t.device != q.device:
+                raise LaError("q, k and v must share dtype and device")
+        self.hk, self.dk, self.hv, self.dv = q.shape[-2], q.shape[-1], v.shape[-2], v.shape[-1]
+        self.lead = tuple(q.shape[:lead])
+        _shape("k", k, q.shape)
+        if tuple(v.shape[:lead]) != self.lead:
+            raise LaError("q and v: the same sequences and tokens are wanted")
+        if self.hk < 1 or self.hv < 1 or self.hv % self.hk:
+            raise LaError("the value heads must be a multiple of the key heads")
+        for name, t in (("g", g), ("beta", beta)):
+            _shape(name, t, self.lead + (self.hv,))
+        _on_gpu(q.device, torch.float32, g=g, beta=beta)
+        self.ld = tuple(_rows(name, t, 2) for name, t in (("q", q), ("k", k), ("v", v)))
+        self.batch, self.tokens = (self.lead + (1,))[:2]
+        if offsets is not None:
+            _on_gpu(q.device, torch.int32, offsets=offsets)
+            if offsets.dim() != 1 or offsets.numel() < 2 or self.lead[0] != 1:
+                raise LaError("offsets: one axis of at least two, with one row of packed tokens, is wanted")
+            self.batch = offsets.numel() - 1
+        self.sizes = (self.dt, self.batch, self.tokens, self.hk, self.hv, self.dk, self.dv)
+        self.states = (self.batch, self.hv, self.dk, self.dv)
+        self.inputs = (_ptr(q), self.ld[0], _ptr(k), self.ld[1], _ptr(v), self.ld[2], _ptr(g), _ptr(beta))
+
+    def scale(self, scale):
+        return float(self.dk ** -0.5 if scale is None else scale)
+
+
+def delta_rule(q, k, v, g, beta, scale=None, initial_state=None, offsets=None, want_state=False, keep=False, out=None, workspace=None):
+    """la_delta_rule: the gated delta rule over whole sequences.  q, k [batch, tokens, hk, dk], v [batch, tokens, hv, dv] (views whose tokens
+    are one distance apart, as of a wider projection, are taken as they are), g (log decay) and beta [batch, tokens, hv] in float32,
+    initial_state [batch, hv, dk, dv] in float32.  ``offsets``: int32 [sequences + 1] on the GPU, with batch = 1: packed sequences of different
+    lengths.  ``scale``: dk ** -0.5 where None.  Returns (o, final state or None, saved or None); ``keep``: what delta_rule_backward takes as
+    ``saved`` instead of running the forward pass again."""
+    d = _Delta(q, k, v, g, beta, offsets)
+    o = torch.empty(v.shape, dtype=v.dtype, device=v.device) if out is None else out
+    _shape("out", o, v.shape)
+    _on_gpu(v.device, v.dtype, out=o)
+    _shape("initial_state", initial_state, d.states)
+    _on_gpu(v.device, torch.float32, initial_state=initial_state)
+    state = torch.empty(d.states, dtype=torch.float32, device=v.device) if want_state else None
+    lib, packed = load(), int(offsets is not None)
+    with _on_device(q):
+        saved = torch.empty(int(lib.la_delta_rule_saved_bytes(*d.sizes, packed)), dtype=torch.uint8, device=v.device) if keep else None
+        buf, wp, wb = (None, 0, 0) if keep else _scratch(workspace, int(lib.la_delta_rule_workspace_bytes(*d.sizes, packed)), q)
+        _check(lib.la_delta_rule(*d.sizes, _ptr(offsets), *d.inputs, d.scale(scale), _ptr(initial_state), _ptr(o), _ptr(state), _ptr(saved),
+                                 saved.numel() if keep else 0, wp, wb, _stream(q)), "la_delta_rule")
+    return o, state, saved
+
+
+def delta_rule_backward(q, k, v, g, beta, o_bar, scale=None, initial_state=None, state_bar=None, offsets=None, saved=None, workspace=None):
+    """la_delta_rule_backward: (q_bar, k_bar, v_bar, g_bar, beta_bar, initial_state_bar) from the gradients of delta_rule's results.
+    initial_state_bar is None where initial_state is.  ``saved``: what delta_rule(..., keep=True) gave for the same arguments."""
+    d = _Delta(q, k, v, g, beta, offsets)
+    _shape("o_bar", o_bar, v.shape)
+    _on_gpu(v.device, v.dtype, o_bar=o_bar)
+    for name, t in (("initial_state", initial_state), ("state_bar", state_bar)):
+        _shape(name, t, d.states)
+        _on_gpu(v.device, torch.float32, **{name: t})
+    _on_gpu(v.device, torch.uint8, saved=saved)
+    new = lambda t, dt=None: torch.empty(t.shape, dtype=dt or t.dtype, device=t.device)  # noqa: E731
+    bars = [new(q), new(k), new(v), new(g), new(beta), None if initial_state is None else new(initial_state)]
+    lib = load()
+    with _on_device(q):
+        need = int(lib.la_delta_rule_backward_workspace_bytes(*d.sizes, int(offsets is not None), int(saved is not None)))
+        buf, wp, wb = _scratch(workspace, need, q)
+        _check(lib.la_delta_rule_backward(*d.sizes, _ptr(offsets), *d.inputs, d.scale(scale), _ptr(initial_state), _ptr(o_bar), _ptr(state_bar),
+                                          _ptr(saved), 0 if saved is None else saved.numel(), *[_ptr(t) for t in bars], wp, wb, _stream(q)),
+               "la_delta_rule_backward")
+    return tuple(bars)
+
+
+def delta_rule_step(q, k, v, g, beta, state, slots=None, scale=None, out=None):
+    """la_delta_rule_step: one token of every sequence: q, k [batch, hk, dk], v [batch, hv, dv], g, beta [batch, hv].  ``state``
+    [rows, hv, dk, dv] in float32 is updated in place; sequence n has row ``slots[n]`` (int32, on the GPU), or n.  A slot outside the rows
+    gives zeros and updates nothing.  Returns o [batch, hv, dv]."""
+    d = _Delta(q, k, v, g, beta, None, lead=1)
+    o = torch.empty(v.shape, dtype=v.dtype, device=v.device) if out is None else out
+    _shape("out", o, v.shape)
+    _on_gpu(v.device, v.dtype, out=o)
+    _shape("state", state, (state.shape[0], d.hv, d.dk, d.dv))
+    _on_gpu(v.device, torch.float32, state=state)
+    _on_gpu(v.device, torch.int32, slots=slots)
+    _shape("slots", slots, (d.batch,))
+    with _on_device(q):
+        _check(load().la_delta_rule_step(d.dt, d.batch, d.hk, d.hv, d.dk, d.dv, *d.inputs, d.scale(scale), _ptr(state), state.shape[0], _ptr(slots),
+                                         _ptr(o), _stream(q)), "la_delta_rule_step")
+    return o
+
+
+def _weights(x, weight, bias):
+    """The la_dtype of weight and bias: x's own, or float32 beside 16 bits."""
+    w = weight if weight is not None else bias
+    dt = x.dtype if w is None else w.dtype
+    if dt != x.dtype and not (dt == torch.float32 and x.element_size() == 2):
+        raise LaError("weight and bias: x's dtype, or float32 beside 16 bits, is wanted")
+    for name, t in (("weight", weight), ("bias", bias)):
+        _shape(name, t, x.shape[-1:])
+        _on_gpu(x.device, dt, **{name: t})
+    return dt
+
+
+def _norm_input(x):
+    if not x.is_cuda:
+        raise LaError("tensors must be on the GPU")
+    if x.dim() < 1:
+        raise LaError("x: at least one axis is wanted")
+    return _layer_dt(x), _batch(x, 1), x.shape[-1], _rows("x", x, 1)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, out=None):
+    """la_layer_norm over the last axis of x (whose rows may be a view's, one distance apart).  Returns (y, mean, rstd), the statistics None
+    unless ``want_stats``: layer_norm_backward takes them."""
+    dt, rows, n, ld = _norm_input(x)
+    wdt = _weights(x, weight, bias)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _shape("out", y, x.shape)
+    _on_gpu(x.device, x.dtype, out=y)
+    stat = torch.float64 if x.dtype == torch.float64 else torch.float32
+    mean, rstd = (torch.empty(x.shape[:-1], dtype=stat, device=x.device) for _ in range(2)) if want_stats else (None, None)
+    with _on_device(x):
+        _check(load().la_layer_norm(dt, _LAYER_TYPES[wdt], rows, n, ld, _ptr(x), _ptr(weight), _ptr(bias), float(eps), _ptr(y), _ptr(mean), _ptr(rstd),
+                                    _stream(x)), "la_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_backward(x, y_bar, mean, rstd, weight=None, want_weights=True, out=None, workspace=None):
+    """la_layer_norm_backward: (x_bar, weight_bar, bias_bar) from layer_norm's input and statistics; the last two None unless
+    ``want_weights``, in weight's dtype (x's where weight is None).  ``out`` may be ``y_bar`` itself."""
+    dt, rows, n, ld = _norm_input(x)
+    wdt = _weights(x, weight, None)
+    _shape("y_bar", y_bar, x.shape)
+    _on_gpu(x.device, x.dtype, y_bar=y_bar)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _shape(name, t, x.shape[:-1])
+        _on_gpu(x.device, torch.float64 if x.dtype == torch.float64 else torch.float32, **{name: t})
+    x_bar = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _shape("out", x_bar, x.shape)
+    _on_gpu(x.device, x.dtype, out=x_bar)
+    wb, bb = (torch.empty(n, dtype=wdt, device=x.device) for _ in range(2)) if want_weights else (None, None)
+    lib = load()
+    with _on_device(x):
+        buf, wp, wbytes = _scratch(workspace, int(lib.la_layer_norm_backward_workspace_bytes(dt, rows, n)), x)
+        _check(lib.la_layer_norm_backward(dt, _LAYER_TYPES[wdt], rows, n, ld, _ptr(x), _ptr(y_bar), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(x_bar),
+                                          _ptr(wb), _ptr(bb), wp, wbytes, _stream(x)), "la_layer_norm_backward")
+    return x_bar, wb, bb
+
+
+def clip_gradients(grads, max_norm, out=None, workspace=None):
+    """la_clip_gradients: scales all tensors of ``grads`` by min(1, max_norm / norm) over all of them, into ``out`` (as many tensors of the same
+    shapes and dtypes) or in place.  Returns the norm before it, on the GPU (float64 where a gradient is, else float32); where it is not finite the
+    gradients are passed on unchanged."""
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if not grads:
+        raise LaError("no gradients")
+    if len(outs) != len(grads):
+        raise LaError("out: as many tensors as gradients are wanted")
+    first = grads[0]
+    if not first.is_cuda:
+        raise LaError("tensors must be on the GPU")
+    count = len(grads)
+    for x, y in zip(grads, outs):
+        if x.device != first.device or not x.is_contiguous():
+            raise LaError("gradients must be contiguous and on the same GPU")
+        _layer_dt(x)
+        if y is not x:
+            _shape("out", y, x.shape)
+            _on_gpu(first.device, x.dtype, out=y)
+    types = (ctypes.c_int * count)(*[_LAYER_TYPES[x.dtype] for x in grads])
+    sizes = (ctypes.c_int64 * count)(*[x.numel() for x in grads])
+    src = (ctypes.c_void_p * count)(*[x.data_ptr() for x in grads])
+    dst = src if out is None else (ctypes.c_void_p * count)(*[y.data_ptr() for y in outs])
+    wide = any(x.dtype == torch.float64 for x in grads)
+    norm = torch.empty((), dtype=torch.float64 if wide else torch.float32, device=first.device)
+    lib = load()
+    with _on_device(first):
+        buf, wp, wb = _scratch(workspace, int(lib.la_clip_gradients_workspace_bytes(count, sizes)), first)
+        _check(lib.la_clip_gradients(count, types, sizes, src, dst, float(max_norm), int(wide), _ptr(norm), wp, wb, _stream(first)),
+               "la_clip_gradients")
+    return norm

@@ -16,7 +16,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libla_mi355x.so")
 HOST = os.path.join(PKG, "_la_host.so")
 
-SOURCES = ["tiny.hip", "tiny_ops.hip", "tiny_rows.hip", "leaf.hip", "small_wave.hip", "trsm_stream.hip", "gemm.hip", "elem.hip", "kalman.hip", "la_api.hip"]
+SOURCES = ["tiny.hip", "tiny_ops.hip", "tiny_rows.hip", "leaf.hip", "small_wave.hip", "trsm_stream.hip", "gemm.hip", "elem.hip", "kalman.hip",
+           "layer_util.hip", "norm.hip", "clip.hip", "delta.hip", "delta_grad.hip", "la_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950",
     "-O3",

@@ -1,0 +1,276 @@
+// The norm over all gradients of a model, and the gradients scaled to a largest norm.
+//
+//   norm = sqrt(sum over all tensors of x^2),   out = x min(1, max_norm / norm);  factor 1 where the norm is not finite (or zero)
+//
+// Two passes over the data, since the factor is known after the first only: bound by memory.  Squares are summed in 64 bits, which no gradient
+// overflows (the squares of float's largest values do in 32), and in an order that depends on the sizes alone.  A launch takes the pointers of up to
+// CLIP_TENSORS tensors among its arguments, so that no table is copied to the device.
+#include <cmath>
+
+#include "layer.hpp"
+#include "lowp.hpp"
+
+namespace la {
+
+constexpr int CLIP_TENSORS = 112;     // (the arguments stay below 4096 bytes)
+constexpr int CLIP_TILE = 8192;       // elements that a block takes at a time
+constexpr int CLIP_BLOCKS = 1024;     // of one launch
+
+struct ClipArgs {
+    const void *src[CLIP_TENSORS];
+    void *dst[CLIP_TENSORS];
+    int64_t n[CLIP_TENSORS];
+    uint32_t first[CLIP_TENSORS + 1];  // the first tile of each tensor in this launch; last: their count
+    uint8_t type[CLIP_TENSORS];
+    int count;
+    int parts;       // partial sums of all launches
+    double *part;    // the whole array
+    int part0;       // where this launch's partial sums start
+    double max_norm;
+    void *norm;      // written by the first launch of the second pass
+    int norm64;
+};
+static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ double block_sum(double x)
+{
+    __shared__ double box[4];
+    x = wave_sum(x);
+    if (threadIdx.x % 64 == 0)
+        box[threadIdx.x / 64] = x;
+    __syncthreads();
+    return box[0] + box[1] + box[2] + box[3];
+}
+
+// The tensor of a tile: the last one whose first tile is not past it.
+__device__ __forceinline__ int tensor_of(const ClipArgs &a, uint32_t tile)
+{
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.first[mid] <= tile)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
+// One tile of a tensor, f(first, count elements at p) in packs of 16 bytes where they start on one, one element at a time before and after.
+// `lead`: elements before the first whole pack of the tensor.
+template <typename T>
+__device__ __forceinline__ double tile_squares(const T *p, int64_t n, uint32_t tile)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const int64_t lead = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T);
+    const int64_t from = tile ? lead + (int64_t)tile * CLIP_TILE : 0, to0 = lead + ((int64_t)tile + 1) * CLIP_TILE, to = to0 < n ? to0 : n;
+    double s = 0;
+    int64_t at = tile ? from : (lead < n ? lead : n);
+    if (!tile && threadIdx.x < at) {
+        const double x = (double)(acc_of<T>)p[threadIdx.x];
+        s += x * x;
+    }
+    const int64_t packs = to > at ? (to - at) / VEC : 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < packs; i += 256) {
+        acc_of<T> v[VEC];
+        load_pack<T, VEC>(p + at + i * VEC, v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            s += (double)v[j] * (double)v[j];
+    }
+    at += packs * VEC;
+    if (at + threadIdx.x < to) {
+        const double x = (double)(acc_of<T>)p[at + threadIdx.x];
+        s += x * x;
+    }
+    return s;
+}
+
+__global__ __launch_bounds__(256) void k_grad_squares(const ClipArgs a)
+{
+    double s = 0;
+    for (uint32_t t = blockIdx.x; t < a.first[a.count]; t += gridDim.x) {
+        const int k = tensor_of(a, t);
+        const uint32_t tile = t - a.first[k];
+        switch (a.type[k]) {
+        case LA_F32: s += tile_squares((const float *)a.src[k], a.n[k], tile); break;
+        case LA_F64: s += tile_squares((const double *)a.src[k], a.n[k], tile); break;
+        case LA_BF16: s += tile_squares((const bf16_t *)a.src[k], a.n[k], tile); break;
+        default: s += tile_squares((const f16_t *)a.src[k], a.n[k], tile); break;
+        }
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0)
+        a.part[a.part0 + blockIdx.x] = s;
+}
+
+template <typename T>
+__device__ __forceinline__ void tile_scale(const T *p, T *q, int64_t n, uint32_t tile, double factor)
+{
+    using A = acc_of<T>;
+    constexpr int VEC = 16 / sizeof(T);
+    const A f = (A)factor;
+    const int64_t lead = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T);
+    const int64_t to0 = lead + ((int64_t)tile + 1) * CLIP_TILE, to = to0 < n ? to0 : n;
+    int64_t at = tile ? lead + (int64_t)tile * CLIP_TILE : 0;
+    if (((uintptr_t)p & 15) != ((uintptr_t)q & 15)) {  // no pack starts on 16 bytes in both
+        for (int64_t i = at + threadIdx.x; i < to; i += 256)
+            q[i] = (T)((A)p[i] * f);
+        return;
+    }
+    if (!tile) {
+        at = lead < n ? lead : n;
+        if (threadIdx.x < at)
+            q[threadIdx.x] = (T)((A)p[threadIdx.x] * f);
+    }
+    const int64_t packs = to > at ? (to - at) / VEC : 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < packs; i += 256) {
+        A v[VEC];
+        load_pack<T, VEC>(p + at + i * VEC, v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            v[j] *= f;
+        store_pack<T, VEC>(q + at + i * VEC, v);
+    }
+    at += packs * VEC;
+    if (at + threadIdx.x < to)
+        q[at + threadIdx.x] = (T)((A)p[at + threadIdx.x] * f);
+}
+
+// Every block sums the partial sums itself, in the same order: no launch in between.
+__global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs a)
+{
+    double s = 0;
+    for (int i = threadIdx.x; i < a.parts; i += 256)
+        s += a.part[i];
+    const double norm = sqrt(block_sum(s));
+    const double factor = norm > a.max_norm && norm < INFINITY ? a.max_norm / norm : 1.0;
+    if (a.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
+        if (a.norm64)
+            *(double *)a.norm = norm;
+        else
+            *(float *)a.norm = (float)norm;
+    }
+    for (uint32_t t = blockIdx.x; t < a.first[a.count]; t += gridDim.x) {
+        const int k = tensor_of(a, t);
+        if (factor == 1.0 && a.src[k] == a.dst[k])
+            continue;
+        const uint32_t tile = t - a.first[k];
+        switch (a.type[k]) {
+        case LA_F32: tile_scale((const float *)a.src[k], (float *)a.dst[k], a.n[k], tile, factor); break;
+        case LA_F64: tile_scale((const double *)a.src[k], (double *)a.dst[k], a.n[k], tile, factor); break;
+        case LA_BF16: tile_scale((const bf16_t *)a.src[k], (bf16_t *)a.dst[k], a.n[k], tile, factor); break;
+        default: tile_scale((const f16_t *)a.src[k], (f16_t *)a.dst[k], a.n[k], tile, factor); break;
+        }
+    }
+}
+
+static int64_t tiles_of(int64_t n) { return n > 0 ? (n + CLIP_TILE - 1) / CLIP_TILE : 0; }
+
+// Calls f(tensors [i, j), their tiles) for each launch: up to CLIP_TENSORS tensors and fewer than 2^31 tiles.
+template <class F>
+static la_status clip_launches(int count, const int64_t *sizes, F &&f)
+{
+    for (int i = 0; i < count;) {
+        int j = i, used = 0;
+        int64_t tiles = 0;
+        while (j < count && used < CLIP_TENSORS && tiles + tiles_of(sizes[j]) < 0x7fffffff) {
+            tiles += tiles_of(sizes[j]);
+            used += sizes[j] > 0;
+            ++j;
+        }
+        if (j == i)
+            return LA_ERR_UNSUPPORTED;  // (one tensor of 2^31 tiles)
+        LA_TRY(f(i, j, tiles));
+        i = j;
+    }
+    return LA_OK;
+}
+
+static int clip_blocks(int64_t tiles) { return (int)(tiles < 1 ? 1 : tiles < CLIP_BLOCKS ? tiles : CLIP_BLOCKS); }
+
+}  // namespace la
+
+using namespace la;
+
+extern "C" {
+
+size_t la_clip_gradients_workspace_bytes(int count, const int64_t *sizes)
+{
+    if (count <= 0 || !sizes)
+        return 0;
+    size_t parts = 0;
+    for (int i = 0; i < count; ++i)
+        if (sizes[i] < 0)
+            return 0;
+    if (clip_launches(count, sizes, [&](int, int, int64_t tiles) {
+            parts += clip_blocks(tiles);
+            return LA_OK;
+        }) != LA_OK)
+        return 0;
+    return align_up(parts * sizeof(double));
+}
+
+la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *sizes, const void *const *grads, void *const *out, double max_norm,
+                            la_dtype norm_type, void *norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (count < 0 || !(max_norm >= 0) || (norm_type != LA_F32 && norm_type != LA_F64) || !norm)
+        return LA_ERR_INVALID_ARG;
+    hipStream_t st = (hipStream_t)stream;
+    if (count == 0)
+        return zero_bytes(norm, bytes_of(norm_type), st);
+    if (!types || !sizes || !grads || !out)
+        return LA_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        if (unknown_dtype(types[i]) || sizes[i] < 0)
+            return LA_ERR_INVALID_ARG;
+        const size_t b = (size_t)sizes[i] * bytes_of(types[i]);
+        if (b && (!grads[i] || !out[i] || (uintptr_t)grads[i] % bytes_of(types[i]) || (uintptr_t)out[i] % bytes_of(types[i]) ||
+                  (grads[i] != out[i] && overlaps(grads[i], b, out[i], b)) || overlaps(norm, bytes_of(norm_type), out[i], b)))
+            return LA_ERR_INVALID_ARG;
+    }
+    const size_t need = la_clip_gradients_workspace_bytes(count, sizes);
+    if (!need)
+        return LA_ERR_UNSUPPORTED;
+    LA_TRY(check_workspace(workspace, workspace_bytes, need, "la_clip_gradients_workspace_bytes"));
+    ClipArgs a;
+    a.part = (double *)workspace;
+    a.max_norm = max_norm;
+    a.norm = norm;
+    a.norm64 = norm_type == LA_F64;
+    a.parts = 0;
+    LA_TRY(clip_launches(count, sizes, [&](int, int, int64_t tiles) {
+        a.parts += clip_blocks(tiles);
+        return LA_OK;
+    }));
+    for (int pass = 0; pass < 2; ++pass) {
+        a.part0 = 0;
+        LA_TRY(clip_launches(count, sizes, [&](int i, int j, int64_t tiles) {
+            a.count = 0;
+            uint32_t at = 0;
+            for (; i < j; ++i) {
+                if (sizes[i] == 0)
+                    continue;
+                a.src[a.count] = grads[i];
+                a.dst[a.count] = out[i];
+                a.n[a.count] = sizes[i];
+                a.type[a.count] = (uint8_t)types[i];
+                a.first[a.count++] = at;
+                at += (uint32_t)tiles_of(sizes[i]);
+            }
+            a.first[a.count] = at;
+            const int blocks = clip_blocks(tiles);
+            if (pass == 0)
+                LA_LAUNCH(k_grad_squares, dim3(blocks), dim3(256), 0, st, a);
+            else
+                LA_LAUNCH(k_grad_scale, dim3(blocks), dim3(256), 0, st, a);
+            a.part0 += blocks;
+            return launch_check("clip");
+        }));
+    }
+    return LA_OK;
+}
+
+}  // extern "C"

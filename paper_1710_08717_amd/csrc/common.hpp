@@ -33,6 +33,7 @@ struct View {
 };
 
 void set_error(hipError_t e, const char *where);
+void set_error_text(const char *text);
 
 #define LA_HIP(call)                         \
     do {                                     \

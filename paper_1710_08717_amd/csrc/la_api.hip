@@ -27,6 +27,8 @@ void set_error(hipError_t e, const char *where)
     snprintf(g_err, sizeof(g_err), "%s: %s", where, hipGetErrorString(e));
 }
 
+void set_error_text(const char *text) { snprintf(g_err, sizeof(g_err), "%s", text); }
+
 // ---------------------------------------------------------------------------------
 // Scratch memory (see common.hpp): the arena of the call that is running on this thread.
 // ---------------------------------------------------------------------------------
