@@ -8,221 +8,398 @@
 //   A_ij = beta_i exp(b_i - b_j) k_i.k_j (j < i),   T = (I + A)^-1,   Z = beta (V - exp(b) K S0),   U = T Z,
 //   P_ij = scale exp(b_i - b_j) q_i.k_j (j <= i),   O = scale exp(b) Q S0 + P U,   S1 = exp(b_last) S0 + K^T exp(b_last - b) U.
 //
-// k_delta_inverse forms T for all chunks at once; k_delta_scan walks a sequence's chunks.  Everything after T is separate for every column of
-// V, so a wavefront takes 16 columns and keeps its part of the state in accumulators from the first chunk to the last.
+// k_delta_pack forms T, P and the operands' packets for all chunks at once; k_delta_scan walks a sequence's chunks.  Everything after T is separate for
+// every column of V, so a wavefront takes 16 columns and keeps its part of the state in accumulators from the first chunk to the last.
 #include "delta.hpp"
 
 namespace la {
 
 // ---------------------------------------------------------------------------------
-// T of every chunk and value head
+// packets of operands, for all chunks at once
 // ---------------------------------------------------------------------------------
-template <typename T, int DKP>
-__global__ __launch_bounds__(64) void k_delta_inverse(DeltaArgs p)
+// One block a chunk and key head.  K Q and K K^T are formed once and stay in accumulators, the decays of every value head are laid over them.  T is
+// formed by blocks: the 16 x 16 blocks of the diagonal by substitution, a column a lane, then twice the lower left block of a 2 x 2 block matrix,
+// -T22 (A21 T11), on the 32-bit matrix instruction.
+template <typename T, int DKP, bool SAVE>
+__global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 {
-    constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI;
-    __shared__ Planes<NI, C, DKP> K;
-    __shared__ __align__(16) float A[C][C + 4];
+    using G = Pack<T, DKP>;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, LD = C + 4;
+    struct Work {
+        float A[C][LD], P[C][LD], inv[C][LD];
+    };
+    union Tiles {
+        char units[G::key_units(SAVE) * UNIT];
+        Work w;
+    };
+    __shared__ __align__(16) Tiles m;
     __shared__ Decays<C> d;
-    const int lane = threadIdx.x, h = blockIdx.x % p.hv;
-    const int64_t slot = blockIdx.x / p.hv;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, x4 = lane >> 4;
+    const int hk = blockIdx.x % p.hk, group = p.hv / p.hk;
+    const int64_t slot = blockIdx.x / p.hk;
     if (p.offsets) {  // tokens of no sequence: zeros
         const int64_t a = p.offsets[0], z = p.offsets[p.batch];
         for (int64_t t = slot * C; t < (slot + 1) * C && t < p.tokens; ++t)
             if (t < a || t >= z)
-                for (int c = lane; c < p.dv; c += 64)
-                    ((T *)p.o)[(t * p.hv + h) * p.dv + c] = (T)0.0f;
+                for (int c = threadIdx.x; c < group * p.dv; c += 256)
+                    ((T *)p.o)[(t * p.hv + hk * group) * p.dv + c] = (T)0.0f;
     }
     int64_t t0;
     int len;
     if (!slot_chunk<C>(p, slot, t0, len))
         return;
-    const int hk = h / (p.hv / p.hk);
-    const T *k = (const T *)p.k + t0 * p.ldk + (int64_t)hk * p.dk;
-    stage_chunk<T, NI, C, DKP, true, false>(k, p.ldk, len, p.dk, &K, nullptr);
-    d.load(p.g + t0 * p.hv + h, p.beta + t0 * p.hv + h, p.hv, len);
-    __syncthreads();
-    const int col = lane & 15, row4 = 4 * (lane >> 4);
+    // 8 x 8 blocks of K and Q: as they are and turned
+    constexpr int UC = DKP / 8, UNITS = (C / 8) * UC;
+    for (int u = threadIdx.x; u < 2 * UNITS; u += 256) {
+        const bool isq = u >= UNITS;
+        const int c = (u % UNITS) % UC, r = (u % UNITS) / UC;
+        const int64_t ld = isq ? p.ldq : p.ldk;
+        const T *src = (const T *)(isq ? p.q : p.k) + (t0 + 8 * r) * ld + (int64_t)hk * p.dk + 8 * c;
+        f32x8 x[8];
 #pragma unroll
-    for (int ti = 0; ti < C / 16; ++ti)
+        for (int i = 0; i < 8; ++i)
+            x[i] = load8<T>(src + i * ld, 8 * r + i < len ? p.dk - 8 * c : 0);
 #pragma unroll
-        for (int tj = 0; tj <= ti; ++tj) {
-            f32x4 x = {0, 0, 0, 0};
+        for (int i = 0; i < 8; ++i) {  // token 8 r + i: row 4 (r % 4) + i % 4 of tile 2 (r / 4) + i / 4
+            const Frag<NI> f = split<NI>(x[i]);
+            char *at = m.units + ((isq ? G::Q : G::K) + G::row(2 * (r >> 2) + (i >> 2), c >> 2)) * UNIT + 16 * (16 * (c & 3) + 4 * (r & 3) + (i & 3));
 #pragma unroll
-            for (int s = 0; s < DKP / 32; ++s)
-                mma(x, K.frag(16 * ti, s), K.frag(16 * tj, s));
-            const int j = 16 * tj + col;
+            for (int k = 0; k < NI; ++k)
+                *reinterpret_cast<bf16x8 *>(at + k * G::FK * UNIT) = f.p[k];
+        }
+        if (!isq || SAVE) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * ti + row4 + r;
-                A[i][j] = j < i ? d.beta[i] * d.between(i, j) * x[r] : 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                const Frag<NI> f = split<NI>(f32x8{x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]});
+                char *at = m.units + ((isq ? G::QTURN : G::KTURN) + G::turned(2 * (c >> 2) + (j >> 2), r >> 2)) * UNIT +
+                           16 * (16 * (r & 3) + 4 * (c & 3) + (j & 3));
+#pragma unroll
+                for (int k = 0; k < NI; ++k)
+                    *reinterpret_cast<bf16x8 *>(at + k * G::FK * UNIT) = f.p[k];
             }
         }
+    }
     __syncthreads();
-    // column `lane` of T by forward substitution
-    float *out = p.inv + (slot * p.hv + h) * C * C;
-    float t[C];
+    char *pk = p.pack_k + (slot * p.hk + hk) * (int64_t)G::key_units(SAVE) * UNIT;
+    for (int u = wave; u < G::key_units(SAVE); u += 4)
+        *reinterpret_cast<bf16x8 *>(pk + u * UNIT + 16 * lane) = *reinterpret_cast<const bf16x8 *>(m.units + u * UNIT + 16 * lane);
+    // row tile `wave` (of C = 32: tiles 0 and 1 by half of the wavefronts each half of the steps) of K K^T and Q K^T
+    constexpr int NT = C == 64 ? RT : 1;  // column tiles of a wavefront
+    const int ti = C == 64 ? wave : wave & 1, tj0 = C == 64 ? 0 : wave >> 1;
+    f32x4 kk[NT], qk[NT];
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        float s[4] = {i == lane ? 1.0f : 0.0f, 0, 0, 0};
+    for (int j = 0; j < NT; ++j) {
+        kk[j] = qk[j] = f32x4{0, 0, 0, 0};
+        if ((tj0 + j) / 2 <= ti / 2) {
 #pragma unroll
-        for (int l = 0; l < i; l += 4) {
-            const f32x4 a = *reinterpret_cast<const f32x4 *>(&A[i][l]);
-#pragma unroll
-            for (int m = 0; m < 4; ++m)
-                if (l + m < i)
-                    s[m] -= a[m] * t[l + m];
+            for (int s = 0; s < G::KS; ++s) {
+                const Frag<NI> f = unit<NI>(m.units, G::K + G::row(tj0 + j, s), G::FK);
+                mma<3>(kk[j], unit<NI>(m.units, G::K + G::row(ti, s), G::FK), f);
+                mma<3>(qk[j], unit<NI>(m.units, G::Q + G::row(ti, s), G::FK), f);
+            }
         }
-        t[i] = (s[0] + s[1]) + (s[2] + s[3]);
-        if (lane < C)
-            out[i * C + lane] = t[i];
+    }
+    const int i0 = first_of(ti);
+    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+        __syncthreads();  // the units (or the head before) are read
+        if (wave == 0)
+            d.load(p.g + t0 * p.hv + h, p.beta + t0 * p.hv + h, p.hv, len);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            if ((tj0 + j) / 2 <= ti / 2) {
+                const int tj = element_of(tj0 + j, col);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = i0 + r;
+                    const float e = d.between(i, tj);
+                    m.w.A[i][tj] = tj < i ? d.beta[i] * e * kk[j][r] : 0.0f;
+                    m.w.P[i][tj] = tj <= i ? p.scale * e * qk[j][r] : 0.0f;
+                }
+            }
+        }
+        __syncthreads();
+        char *pv = p.pack_v + (slot * p.hv + h) * (int64_t)G::value_units(SAVE) * UNIT;
+        if (wave == 0) {  // the blocks of the diagonal
+            const int b0 = 16 * x4;
+            if (b0 < C) {
+                float t[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float s[2] = {i == col ? 1.0f : 0.0f, 0};
+#pragma unroll
+                    for (int l = 0; l < i; l += 4) {
+                        const f32x4 a = *reinterpret_cast<const f32x4 *>(&m.w.A[b0 + i][b0 + l]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (l + k < i)
+                                s[k & 1] -= a[k] * t[l + k];
+                    }
+                    t[i] = s[0] + s[1];
+                    m.w.inv[b0 + i][b0 + col] = t[i];
+                }
+            }
+        } else {  // the others meanwhile: P and the decays out, zeros right of the diagonal
+            for (int u = wave - 1; u < (SAVE ? 2 : 1) * G::FT; u += 3) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int s = 0; s < G::CS; ++s) {
+                        if (s <= i / 2 && u == G::lower(i, s)) {
+                            const float *row = &m.w.P[element_of(i, col)][32 * s + 8 * x4];
+                            put_unit<G::NO>(pv, G::P + u, G::FT, join(*reinterpret_cast<const f32x4 *>(row), *reinterpret_cast<const f32x4 *>(row + 4)));
+                        }
+                        if (SAVE && s >= i / 2 && u == G::FT + G::upper(i, s)) {
+                            f32x8 x;
+#pragma unroll
+                            for (int r = 0; r < 8; ++r)
+                                x[r] = m.w.P[32 * s + 8 * x4 + r][element_of(i, col)];
+                            put_unit<NX>(pv, G::PTURN + u - G::FT, G::FT, x);
+                        }
+                    }
+            }
+            if (wave < 3)
+                *reinterpret_cast<f32x4 *>(pv + (wave - 1) * UNIT + 16 * lane) = *reinterpret_cast<const f32x4 *>((const char *)&d + (wave - 1) * UNIT + 16 * lane);
+            else
+                for (int b = 0; b < C; b += 32)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        m.w.inv[b + 4 * x4 + r][b + 16 + col] = 0.0f;
+        }
+        __syncthreads();
+        if (wave < C / 32) {
+            const int b = 32 * wave;
+            f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x = __builtin_amdgcn_mfma_f32_16x16x4f32(m.w.A[b + 16 + col][b + 4 * k + x4], m.w.inv[b + 4 * k + x4][b + col], x, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                y = __builtin_amdgcn_mfma_f32_16x16x4f32(m.w.inv[b + 16 + col][b + 16 + 4 * x4 + r], x[r], y, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                m.w.inv[b + 16 + 4 * x4 + r][b + col] = -y[r];
+        }
+        if constexpr (C == 64) {
+            __syncthreads();
+            const int a1 = wave >> 1, b = 16 * (wave & 1);  // block row of T22, block column of T11
+            f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+                if (a <= a1) {
+                    f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)  // (the upper right block of T11 is zero)
+                        x = __builtin_amdgcn_mfma_f32_16x16x4f32(m.w.A[32 + 16 * a + col][4 * k + x4], m.w.inv[4 * k + x4][b + col], x, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        y = __builtin_amdgcn_mfma_f32_16x16x4f32(m.w.inv[32 + 16 * a1 + col][32 + 16 * a + 4 * x4 + r], x[r], y, 0, 0, 0);
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                m.w.inv[32 + 16 * a1 + 4 * x4 + r][b + col] = -y[r];
+        }
+        __syncthreads();
+        for (int u = wave; u < (SAVE ? 2 : 1) * G::FT; u += 4) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int s = 0; s < G::CS; ++s) {
+                    if (s <= i / 2 && u == G::lower(i, s)) {
+                        const float *row = &m.w.inv[element_of(i, col)][32 * s + 8 * x4];
+                        put_unit<NX>(pv, G::TINV + u, G::FT, join(*reinterpret_cast<const f32x4 *>(row), *reinterpret_cast<const f32x4 *>(row + 4)));
+                    }
+                    if (SAVE && s >= i / 2 && u == G::FT + G::upper(i, s)) {
+                        f32x8 x;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            x[r] = m.w.inv[32 * s + 8 * x4 + r][element_of(i, col)];
+                        put_unit<NX>(pv, G::TTURN + u - G::FT, G::FT, x);
+                    }
+                }
+        }
     }
 }
 
 // ---------------------------------------------------------------------------------
 // the walk over a sequence's chunks
 // ---------------------------------------------------------------------------------
+// A chunk has two halves: Z and U from K, Q, T and the decays, then the answers and the new state from P and Kt.  The first half's packets of the next chunk
+// and the second half's of this one come straight to LDS while the first half runs.
 template <typename T, int DKP, int NW, bool SAVE>
 __global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
 {
-    constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI, RT = C / 16, KT = DKP / 16;
-    struct Tiles {
-        Planes<NI, C, DKP> K, Q;
-        Planes<NI, DKP, C> Kt;
-        Planes<NX, C, C> inv, P;
-        Decays<C> d;
-    };
-    __shared__ __align__(16) Tiles m;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, row4 = 4 * (lane >> 4);
+    using G = Pack<T, DKP>;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, KT = G::KT;
+    // first half: K and Q, one unit of decays, T; second half: Kt, P
+    constexpr int LQ = NI * G::FK, LD = 2 * NI * G::FK, LT = LD + 1, FIRST = LT + NX * G::FT, LP = NI * G::FK, SECOND = LP + G::NO * G::FT;
+    constexpr int EACH1 = share<LD, NW>() + share<FIRST - LD, NW>();
+    using In = RowsIn<T, C, NW>;
+    __shared__ __align__(16) char first[2][FIRST * UNIT];
+    __shared__ __align__(16) char second[SECOND * UNIT];
+    __shared__ __align__(16) char vin[C * 16 * NW * sizeof(T)];
+    __shared__ __align__(16) char turn[NW][C * RowsOut<float, C>::ROW];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
     const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
     const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int c0 = (slice * NW + wave) * 16 + col;  // this lane's column of V
-    const bool live = c0 < p.dv;
+    const int cbase = (slice * NW + wave) * 16, c0 = cbase + col;  // this lane's column of V
+    const bool live = c0 < p.dv, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
     const int hk = h / (p.hv / p.hk);
     const int64_t state_at = (n * p.hv + h) * p.dk * (int64_t)p.dv;
+    const int64_t slot0 = first_slot<C>(p, n, t0);
+    const int chunks = (int)((len + C - 1) / C);
+    const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(SAVE) * UNIT), *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(SAVE) * UNIT);
+    const int64_t key_step = (int64_t)p.hk * (G::key_units(SAVE) * UNIT), value_step = (int64_t)p.hv * (G::value_units(SAVE) * UNIT);
+    const uint32_t first_at = lds_address(first), second_at = lds_address(second);
+    // (pk, pv: the packets of the chunk that is fetched first)
+    auto fetch_first = [&](const char *k, const char *v, int buffer) {
+        stream_run<LD, NW>(k, first_at + buffer * (FIRST * UNIT), wave);
+        stream_run<FIRST - LD, NW>(v + UNIT, first_at + buffer * (FIRST * UNIT) + LD * UNIT, wave);
+    };
+    auto fetch_second = [&](const char *k, const char *v) {
+        stream_run<LP, NW>(k + G::KTURN * UNIT, second_at, wave);
+        stream_run<SECOND - LP, NW>(v + G::P * UNIT, second_at + LP * UNIT, wave);
+    };
+    char *mine = turn[wave];
+    In V;
+    auto fetch_v = [&](int c) {
+        V.fetch((const T *)p.v + (t0 + (int64_t)c * C) * p.ldv + (int64_t)h * p.dv + slice * NW * 16, p.ldv, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                p.dv - slice * NW * 16);
+    };
+    auto keep_state = [&](int c, const f32x4 *S) {
+        if (kept) {
+            float *dst = p.chunk_state + ((slot0 + c) * p.hv + h) * DKP * (int64_t)p.dvp + cbase;
+#pragma unroll
+            for (int i = 0; i < KT / RT; ++i)
+                RowsOut<float, C>::store(mine, dst + (int64_t)i * C * p.dvp, p.dvp, S + i * RT, C, 16);
+        }
+    };
 
     f32x4 S[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 16 * t + row4 + r;
+            const int i = first_of(t) + r;
             S[t][r] = p.state0 && live && i < p.dk ? p.state0[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
-    // the halves of 32-wide steps that lie right of the diagonal stay zero
-    for (int i = threadIdx.x; i < C * Planes<NX, C, C>::LD; i += 64 * NW)
-        for (int x = 0; x < NX; ++x)
-            (&m.P.e[x][0][0])[i] = (bf16_t)0.0f;
-
-    int64_t slot = first_slot<C>(p, n, t0);
-    for (int64_t c = 0; c * C < len; ++c, ++slot) {
-        const int64_t t = t0 + c * C;
-        const int left = (int)(len - c * C < C ? len - c * C : C);
-        __syncthreads();  // the tiles of the chunk before are read
-        stage_chunk<T, NI, C, DKP, true, true>((const T *)p.k + t * p.ldk + (int64_t)hk * p.dk, p.ldk, left, p.dk, &m.K, &m.Kt);
-        stage_chunk<T, NI, C, DKP, true, false>((const T *)p.q + t * p.ldq + (int64_t)hk * p.dk, p.ldq, left, p.dk, &m.Q, nullptr);
-        const float *inv = p.inv + (slot * p.hv + h) * C * C;
-        for (int u = threadIdx.x; u < C * C / 4; u += 64 * NW)
-            m.inv.put4(u / (C / 4), 4 * (u % (C / 4)), *reinterpret_cast<const f32x4 *>(inv + 4 * u));
-        if (wave == 0)
-            m.d.load(p.g + t * p.hv + h, p.beta + t * p.hv + h, p.hv, left);
-        f32x4 V[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + row4 + r;
-                V[i][r] = live && row < left ? (float)((const T *)p.v)[(t + row) * p.ldv + (int64_t)h * p.dv + c0] : 0.0f;
-            }
-        __syncthreads();
-        // P, turned: lane's column is the query, its four rows the keys
-        for (int i = wave; i < RT; i += NW)
-            for (int j = 0; j <= i; ++j) {
-                f32x4 x = {0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < DKP / 32; ++s)
-                    mma(x, m.K.frag(16 * j, s), m.Q.frag(16 * i, s));
-                const int qi = 16 * i + col;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int kj = 16 * j + row4 + r;
-                    x[r] = kj <= qi ? p.scale * m.d.between(qi, kj) * x[r] : 0.0f;
-                }
-                m.P.put4(qi, 16 * j + row4, x);
-            }
-        if constexpr (SAVE) {
-            float *out = p.chunk_state + (slot * p.hv + h) * DKP * (int64_t)p.dvp + c0;
-            if (c0 < p.dvp) {
-#pragma unroll
-                for (int i = 0; i < KT; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        out[(int64_t)(16 * i + row4 + r) * p.dvp] = S[i][r];
-            }
-        }
+    if (chunks > 0) {
+        fetch_first(pk, pv, 0);
+        fetch_v(0);
+        if constexpr (SAVE)
+            keep_state(0, S);
+        V.put(vin);
+        wait_loads<0>();
+    }
+    for (int c = 0; c < chunks; ++c, pk += key_step, pv += value_step) {
+        const char *a = first[c & 1];
+        const bool more = c + 1 < chunks;
+        block_barrier();  // the first half's packets and V are there, the chunk before is read
         f32x4 X[RT], Y[RT], U[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            X[i] = Y[i] = U[i] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < RT; ++i) {
 #pragma unroll
-        for (int s = 0; s < DKP / 32; ++s) {
-            const Frag<NX> f = split<NX>(join(S[2 * s], S[2 * s + 1]));
+            for (int r = 0; r < 4; ++r)
+                U[i][r] = In::at(vin, first_of(i) + r, 16 * wave + col);
+            X[i] = Y[i] = f32x4{0, 0, 0, 0};
+        }
+        Frag<NI> kf[2][RT], qf[2][RT];
+        Frag<NX> tf[G::FT];
+        auto rows_of = [&](int s, Frag<NI> *k, Frag<NI> *q) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                mma(X[i], m.K.frag(16 * i, s), f);
-                mma(Y[i], m.Q.frag(16 * i, s), f);
+                k[i] = unit<NI>(a, G::row(i, s), G::FK);
+                q[i] = unit<NI>(a, LQ + G::row(i, s), G::FK);
             }
+        };
+        rows_of(0, kf[0], qf[0]);
+        issue_point();
+        fetch_second(pk, pv);
+        if (more)
+            fetch_first(pk + key_step, pv + value_step, ~c & 1);
+        Frag<NX> f = split<NX>(join(S[0], S[1]));
+#pragma unroll
+        for (int s = 0; s < G::KS; ++s) {
+            if (s + 1 < G::KS) {
+                rows_of(s + 1, kf[~s & 1], qf[~s & 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < G::FT; ++i)
+                    tf[i] = unit<NX>(a, LT + i, G::FT);
+            }
+            issue_point();
+            const Frag<NX> now = f;
+            if (s + 1 < G::KS)
+                f = split<NX>(join(S[2 * s + 2], S[2 * s + 3]));
+            mma_tiles<3, RT>(X, kf[s & 1], now);
+            mma_tiles<G::NO, RT>(Y, qf[s & 1], now);
         }
+        const Decays<C> &d = *reinterpret_cast<const Decays<C> *>(a + (LD - 1) * UNIT);  // (its second unit)
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const f32x4 in = m.d.four(m.d.in, 16 * i + row4), beta = m.d.four(m.d.beta, 16 * i + row4);
-            X[i] = beta * (V[i] - in * X[i]);  // Z
+            const f32x4 in = d.four(d.in, first_of(i)), beta = d.four(d.beta, first_of(i));
+            X[i] = beta * (U[i] - in * X[i]);  // Z
             Y[i] *= p.scale * in;
+            U[i] = f32x4{0, 0, 0, 0};
         }
-#pragma unroll
-        for (int s = 0; s < C / 32; ++s) {
-            const Frag<NX> f = split<NX>(join(X[2 * s], X[2 * s + 1]));
-#pragma unroll
-            for (int i = 2 * s; i < RT; ++i)
-                mma(U[i], m.inv.frag(16 * i, s), f);
+        mma_tiles<3, (RT < 4 ? RT : 2)>(U, tf, split<NX>(join(X[0], X[1])));
+        if constexpr (RT == 4) {
+            const Frag<NX> f0 = split<NX>(join(X[0], X[1]));
+            const Frag<NX> t2[2] = {tf[2], tf[4]}, t3[2] = {tf[3], tf[5]};
+            mma_tiles<3, 2>(U + 2, t2, f0);
+            mma_tiles<3, 2>(U + 2, t3, split<NX>(join(X[2], X[3])));
         }
-        if constexpr (SAVE) {
-            float *out = p.chunk_u + (slot * p.hv + h) * C * (int64_t)p.dvp + c0;
-            if (c0 < p.dvp) {
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        out[(int64_t)(16 * i + row4 + r) * p.dvp] = U[i][r];
-            }
-        }
-        __syncthreads();  // P is there
-        const float all = m.d.all;
+        const float all = d.all;
 #pragma unroll
         for (int i = 0; i < KT; ++i)
             S[i] *= all;
+        f32x4 out[RT];
 #pragma unroll
-        for (int s = 0; s < C / 32; ++s) {
-            const Frag<NX> f = split<NX>(join(U[2 * s], U[2 * s + 1]));
+        for (int i = 0; i < RT; ++i)
+            out[i] = d.four(d.out, first_of(i));
+        if (more)
+            wait_loads<EACH1>();
+        else
+            wait_loads<0>();
+        block_barrier();  // the second half's packets are there, V is read
+        if (more)
+            fetch_v(c + 1);
+        Frag<G::NO> pf[G::FT];
+        Frag<NI> ktf[2][KT];
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+            ktf[0][i] = unit<NI>(second, G::turned(i, 0), G::FK);
+#pragma unroll
+        for (int i = 0; i < G::FT; ++i)
+            pf[i] = unit<G::NO>(second, LP + i, G::FT);
+        issue_point();
+#pragma unroll
+        for (int s = 0; s < G::CS; ++s) {
+            if (s + 1 < G::CS) {
+#pragma unroll
+                for (int i = 0; i < KT; ++i)
+                    ktf[~s & 1][i] = unit<NI>(second, G::turned(i, s + 1), G::FK);
+                issue_point();
+            }
+            mma_tiles<3, KT>(S, ktf[s & 1], split<NX>(join(U[2 * s] * out[2 * s], U[2 * s + 1] * out[2 * s + 1])));
+            const Frag<NX> u = split<NX>(join(U[2 * s], U[2 * s + 1]));
 #pragma unroll
             for (int i = 2 * s; i < RT; ++i)
-                mma(Y[i], m.P.frag(16 * i, s), f);
-            const Frag<NX> w = split<NX>(join(U[2 * s] * m.d.four(m.d.out, 32 * s + row4), U[2 * s + 1] * m.d.four(m.d.out, 32 * s + 16 + row4)));
-#pragma unroll
-            for (int i = 0; i < KT; ++i)
-                mma(S[i], m.Kt.frag(16 * i, s), w);
+                mma<G::NO>(Y[i], pf[G::lower(i, s)], u);
         }
-        if (live) {
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * i + row4 + r;
-                    if (row < left)
-                        ((T *)p.o)[((t + row) * p.hv + h) * p.dv + c0] = (T)Y[i][r];
-                }
+        wait_loads<0>();  // (before the stores: the next chunk does not wait for them)
+        if (more)
+            V.put(vin);
+        const int64_t t = t0 + (int64_t)c * C;
+        const int left = (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C);
+        RowsOut<T, C>::store(mine, (T *)p.o + (t * p.hv + h) * p.dv + cbase, (int64_t)p.hv * p.dv, Y, left, p.dv - cbase);
+        if constexpr (SAVE) {
+            if (kept)
+                RowsOut<float, C>::store(mine, p.chunk_u + ((slot0 + c) * p.hv + h) * C * (int64_t)p.dvp + cbase, p.dvp, U, C, 16);
+            if (more)
+                keep_state(c + 1, S);
         }
     }
     if (p.state1 && live) {
@@ -230,26 +407,27 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + row4 + r;
+                const int i = first_of(t) + r;
                 if (i < p.dk)
                     p.state1[state_at + (int64_t)i * p.dv + c0] = S[t][r];
             }
     }
 }
 
-template <typename T, int DKP>
-static la_status scan_t(DeltaArgs &p, bool save, hipStream_t st)
+template <typename T, int DKP, bool SAVE>
+static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
     constexpr int NW = 4;
     if (p.slots > 0)
-        LA_LAUNCH((k_delta_inverse<T, DKP>), dim3((unsigned)(p.slots * p.hv)), dim3(64), 0, st, p);
+        LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
     p.slices = (p.dv + 16 * NW - 1) / (16 * NW);
-    const dim3 grid((unsigned)(p.batch * p.hv * p.slices));
-    if (save)
-        LA_LAUNCH((k_delta_scan<T, DKP, NW, true>), grid, dim3(64 * NW), 0, st, p);
-    else
-        LA_LAUNCH((k_delta_scan<T, DKP, NW, false>), grid, dim3(64 * NW), 0, st, p);
+    LA_LAUNCH((k_delta_scan<T, DKP, NW, SAVE>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(64 * NW), 0, st, p);
     return launch_check("delta rule");
+}
+template <typename T, int DKP>
+static la_status scan_t(DeltaArgs &p, bool save, hipStream_t st)
+{
+    return save ? scan_s<T, DKP, true>(p, st) : scan_s<T, DKP, false>(p, st);
 }
 
 la_status launch_delta_rule(la_dtype dt, DeltaArgs p, bool save, hipStream_t st)
@@ -373,16 +551,30 @@ static la_status step_t(DeltaStepArgs &p, int64_t batch, hipStream_t st)
 // sizes and buffers
 // ---------------------------------------------------------------------------------
 constexpr int DELTA_MAX_DK = 128, DELTA_MAX_DV = 1024;
-
-static int chunk_of(la_dtype dt) { return dt == LA_BF16 ? DeltaIn<bf16_t>::C : dt == LA_F16 ? DeltaIn<f16_t>::C : DeltaIn<float>::C; }
+constexpr int64_t DELTA_MAX_ROW = 1 << 24;  // elements of one token's row of v
 
 struct DeltaSizes {
     int64_t slots = 0, all = 0;  // chunks, tokens of all sequences
     int c = 0, dkp = 0, dvp = 0;
-    size_t inv = 0, state = 0, u = 0;  // bytes of the arrays by slot and value head
-    size_t saved() const { return inv + state + u; }
+    size_t key[2] = {}, value[2] = {};  // bytes of the packets, without and with what the gradient takes
+    size_t state = 0, u = 0;            // of the states and of U by slot and value head
+    size_t packets(bool save) const { return key[save] + value[save]; }
+    size_t saved() const { return packets(true) + state + u; }
     size_t grad() const { return state + u; }  // the state's gradient, Z's gradient
 };
+
+template <typename T, int DKP>
+static void packet_sizes(DeltaSizes &z, bool packed, int64_t batch, int64_t tokens, int hk, int hv)
+{
+    using G = Pack<T, DKP>;
+    z.c = G::C;
+    z.dkp = DKP;
+    z.slots = batch == 0 ? 0 : packed ? tokens / z.c + batch : batch * ((tokens + z.c - 1) / z.c);
+    for (int save = 0; save < 2; ++save) {
+        z.key[save] = (size_t)z.slots * hk * G::key_units(save) * UNIT;
+        z.value[save] = (size_t)z.slots * hv * G::value_units(save) * UNIT;
+    }
+}
 
 static la_status delta_sizes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, bool packed, DeltaSizes &z)
 {
@@ -393,26 +585,33 @@ static la_status delta_sizes(la_dtype dt, int64_t batch, int64_t tokens, int hk,
     constexpr int64_t most = 0x7fffffff;
     if (batch > most || tokens > most || (!packed && batch && tokens > most / batch))
         return LA_ERR_UNSUPPORTED;
-    z.c = chunk_of(dt);
-    z.dkp = dk <= 64 ? 64 : 128;
+    const bool half = dk <= 64;
+    if (dt == LA_F32)
+        half ? packet_sizes<float, 64>(z, packed, batch, tokens, hk, hv) : packet_sizes<float, 128>(z, packed, batch, tokens, hk, hv);
+    else if (dt == LA_BF16)
+        half ? packet_sizes<bf16_t, 64>(z, packed, batch, tokens, hk, hv) : packet_sizes<bf16_t, 128>(z, packed, batch, tokens, hk, hv);
+    else
+        half ? packet_sizes<f16_t, 64>(z, packed, batch, tokens, hk, hv) : packet_sizes<f16_t, 128>(z, packed, batch, tokens, hk, hv);
     z.dvp = (dv + 31) / 32 * 32;
     z.all = packed ? tokens : batch * tokens;
-    z.slots = batch == 0 ? 0 : packed ? tokens / z.c + batch : batch * ((tokens + z.c - 1) / z.c);
+    if ((int64_t)hv * dv > DELTA_MAX_ROW)  // lanes address 24 rows by 32 bits
+        return LA_ERR_UNSUPPORTED;
     if (z.slots > most / hv || batch > most / hv / ((dv + 15) / 16))  // blocks of one launch
         return LA_ERR_UNSUPPORTED;
     const size_t heads = (size_t)z.slots * hv;
-    z.inv = align_up(heads * z.c * z.c * 4);
     z.state = align_up(heads * z.dkp * z.dvp * 4);
     z.u = align_up(heads * z.c * z.dvp * 4);
     return LA_OK;
 }
 
-static void place_saved(DeltaArgs &p, const DeltaSizes &z, void *base)
+static void place_packets(DeltaArgs &p, const DeltaSizes &z, void *base, bool save)
 {
-    char *at = (char *)base;
-    p.inv = (float *)at;
-    p.chunk_state = (float *)(at + z.inv);
-    p.chunk_u = (float *)(at + z.inv + z.state);
+    p.pack_k = (char *)base;
+    p.pack_v = p.pack_k + z.key[save];
+    if (save) {
+        p.chunk_state = (float *)(p.pack_v + z.value[save]);
+        p.chunk_u = (float *)((char *)p.chunk_state + z.state);
+    }
 }
 
 la_status launch_delta_backward(la_dtype dt, DeltaArgs p, hipStream_t st);
@@ -426,7 +625,7 @@ extern "C" {
 size_t la_delta_rule_workspace_bytes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, int packed)
 {
     DeltaSizes z;
-    return delta_sizes(dt, batch, tokens, hk, hv, dk, dv, packed, z) == LA_OK ? z.inv : 0;
+    return delta_sizes(dt, batch, tokens, hk, hv, dk, dv, packed, z) == LA_OK ? z.packets(false) : 0;
 }
 
 size_t la_delta_rule_saved_bytes(la_dtype dt, int64_t batch, int64_t tokens, int hk, int hv, int dk, int dv, int packed)
@@ -452,6 +651,8 @@ la_status la_delta_rule(la_dtype dt, int64_t batch, int64_t tokens, int hk, int 
         return offsets && z.all ? LA_ERR_INVALID_ARG : LA_OK;
     if (ldq < (int64_t)hk * dk || ldk < (int64_t)hk * dk || ldv < (int64_t)hv * dv)
         return LA_ERR_INVALID_ARG;
+    if (ldv > DELTA_MAX_ROW)
+        return LA_ERR_UNSUPPORTED;
     const size_t es = bytes_of(dt), ob = (size_t)z.all * hv * dv * es, sb = (size_t)batch * hv * dk * dv * 4;
     if (z.all && (!q || !k || !v || !g || !beta || !o))
         return LA_ERR_INVALID_ARG;
@@ -465,12 +666,12 @@ la_status la_delta_rule(la_dtype dt, int64_t batch, int64_t tokens, int hk, int 
     p.slots = z.slots;
     p.dvp = z.dvp;
     void *base = saved ? saved : workspace;
-    const size_t need = saved ? z.saved() : z.inv, given = saved ? saved_bytes : workspace_bytes;
+    const size_t need = saved ? z.saved() : z.packets(false), given = saved ? saved_bytes : workspace_bytes;
     LA_TRY(check_workspace(base, given, need, saved ? "la_delta_rule_saved_bytes" : "la_delta_rule_workspace_bytes"));
     if (overlaps(base, need, q, qs) || overlaps(base, need, k, ks) || overlaps(base, need, v, vs) || overlaps(base, need, o, ob) ||
         overlaps(base, need, state, sb) || overlaps(base, need, initial_state, sb) || overlaps(base, need, g, gs) || overlaps(base, need, beta, gs))
         return LA_ERR_INVALID_ARG;
-    place_saved(p, z, base);
+    place_packets(p, z, base, saved != nullptr);
     return launch_delta_rule(dt, p, saved != nullptr, (hipStream_t)stream);
 }
 
@@ -486,6 +687,8 @@ la_status la_delta_rule_backward(la_dtype dt, int64_t batch, int64_t tokens, int
         return offsets && z.all ? LA_ERR_INVALID_ARG : LA_OK;
     if (ldq < (int64_t)hk * dk || ldk < (int64_t)hk * dk || ldv < (int64_t)hv * dv)
         return LA_ERR_INVALID_ARG;
+    if (ldv > DELTA_MAX_ROW)
+        return LA_ERR_UNSUPPORTED;
     if (z.all && (!q || !k || !v || !g || !beta || !o_bar || !q_bar || !k_bar || !v_bar || !g_bar || !beta_bar))
         return LA_ERR_INVALID_ARG;
     const size_t es = bytes_of(dt), ob = (size_t)z.all * hv * dv * es, qb = (size_t)z.all * hk * dk * es, gb = (size_t)z.all * hv * 4,
@@ -525,9 +728,9 @@ la_status la_delta_rule_backward(la_dtype dt, int64_t batch, int64_t tokens, int
     p.chunk_z_bar = (float *)(at + z.state);
     at += z.grad();
     if (saved) {
-        place_saved(p, z, (void *)saved);
+        place_packets(p, z, (void *)saved, true);
     } else {  // the forward pass again; its answers go to scratch
-        place_saved(p, z, at);
+        place_packets(p, z, at, true);
         p.o = at + z.saved();
         LA_TRY(launch_delta_rule(dt, p, true, st));
     }

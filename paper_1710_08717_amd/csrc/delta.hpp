@@ -1,14 +1,14 @@
-// Pieces of the gated delta rule's kernels (delta.hip, delta_grad.hip): operands on the matrix cores, tiles in LDS, sequences and chunks.
+// Pieces of the gated delta rule's kernels (delta.hip, delta_grad.hip): operands on the matrix cores, packets of them, sequences and chunks.
 //
 // Products run on the bf16 matrix instruction (16 x 16 x 32) at the precision of 32 bits: a number x is the sum of up to three bf16 pieces
 // (x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1): 24 bits), a product of two numbers the sum of the products of pieces i, j with
 // i + j < 3.  An input in bf16 is one piece, in f16 two, in f32 three; what the kernels compute is three.  That is 3 instructions for bf16 input
 // times a computed operand and 6 for two computed ones, against the 16 that the 32-bit matrix instruction takes in time.
 //
-// The accumulator of a 16 x 16 tile has, in lane l, column l % 16 and rows 4 (l / 16) .. + 3; an operand of 32 summed elements has, in lane l, row
-// (or column) l % 16 and 8 elements.  Since the order of summation is free, the two tiles of rows 32 s .. 32 s + 31 of an accumulator ARE the operand of
-// step s, if the other operand takes its 8 elements in the same order: 32 s + 4 (l / 16) .. + 3 and 16 more .. + 3.  Tiles in LDS are kept in that order
-// (slot_of), so that no accumulator passes through LDS on its way into the next product.
+// An operand of 32 summed elements has, in lane l, row (or column) l % 16 and elements 8 (l / 16) .. + 7; the accumulator of a 16 x 16 tile has column
+// l % 16 and rows 4 (l / 16) .. + 3.  Which token or key element a tile's row stands for is free, so row 4 x + r of tile 2 s + y is taken to be element
+// 32 s + 8 x + 4 y + r: then tiles 2 s and 2 s + 1 of an accumulator ARE the operand of step s, and no accumulator passes through LDS on its way into
+// the next product.
 #pragma once
 #include "layer.hpp"
 #include "lowp.hpp"
@@ -33,10 +33,11 @@ struct DeltaArgs {
     float scale;
     void *o;
     float *state1;  // final states or null
-    // by chunk slot and value head: the inverses T [C][C], and for the gradient the state before the chunk [DKP][dvp] and U [C][dvp]
-    float *inv, *chunk_state, *chunk_u;
-    int64_t slots;
-    int dvp;  // dv rounded up to whole tiles
+    int64_t slots;  // chunks
+    int dvp;        // dv rounded up to whole steps
+    // by chunk slot: packets of operands for every key head and every value head; for the gradient the state before the chunk [DKP][dvp] and U [C][dvp]
+    char *pack_k, *pack_v;
+    float *chunk_state, *chunk_u;
     // gradient
     const void *o_bar;
     const float *state1_bar;
@@ -68,17 +69,34 @@ struct Frag {
     bf16x8 p[N];
 };
 
-// d += a b, products of the smallest pieces first
-template <int NA, int NB>
+// d += a b: products of pieces i, j with i + j < LIM, the smallest first
+template <int LIM, int NA, int NB>
 __device__ __forceinline__ void mma(f32x4 &d, const Frag<NA> &a, const Frag<NB> &b)
 {
 #pragma unroll
-    for (int s = 2; s >= 0; --s)
+    for (int s = LIM - 1; s >= 0; --s)
 #pragma unroll
         for (int i = 0; i < NA; ++i)
             if (s - i >= 0 && s - i < NB)
                 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], d, 0, 0, 0);
 }
+
+// the same for N tiles with one operand in common, tile after tile: no instruction waits for the one before it
+template <int LIM, int N, int NA, int NB>
+__device__ __forceinline__ void mma_tiles(f32x4 *d, const Frag<NA> *a, const Frag<NB> &b)
+{
+#pragma unroll
+    for (int s = LIM - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    d[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n].p[i], b.p[s - i], d[n], 0, 0, 0);
+            }
+}
+// keeps what is before it (loads of operands) before what follows: the compiler moves loads down to their use, where they would be waited for
+__device__ __forceinline__ void issue_point() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int N>
 __device__ __forceinline__ Frag<N> split(f32x8 x)
@@ -94,49 +112,117 @@ __device__ __forceinline__ Frag<N> split(f32x8 x)
 }
 __device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// where element c of a row (or the first of four from a multiple of four) lies in an LDS tile
-__device__ __forceinline__ int slot_of(int c)
+// the element that row m of tile i stands for; the first of the four that a lane's accumulator of tile i holds
+__device__ __forceinline__ int element_of(int i, int m) { return 32 * (i >> 1) + 8 * (m >> 2) + 4 * (i & 1) + (m & 3); }
+__device__ __forceinline__ int first_of(int i) { return 32 * (i >> 1) + 8 * ((threadIdx.x & 63) >> 4) + 4 * (i & 1); }
+
+// Operands of one chunk in the order in which a wavefront reads them: 1024 bytes (16 a lane) for 16 rows, 32 summed elements and one piece, "a unit".
+//   key head:   K (rows tokens, summed over dk), Q, and turned (rows dk, summed over tokens) Kt, for the gradient also Qt
+//   value head: decays (2 units), T and P (lower triangles: steps s <= i / 2 of row tile i), for the gradient also T^T and P^T (s >= i / 2)
+constexpr int UNIT = 1024;
+template <typename T, int DKP>
+struct Pack {
+    static constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI;
+    static constexpr int RT = C / 16, KS = DKP / 32, KT = DKP / 16, CS = C / 32;
+    static constexpr int NO = NI == 3 ? 3 : 2;  // pieces of what only the answers take: they are rounded to the input's type
+    static constexpr int FK = RT * KS, FT = CS == 1 ? 2 : 6;
+    static constexpr int K = 0, Q = NI * FK, KTURN = 2 * NI * FK, QTURN = 3 * NI * FK;
+    static constexpr int D = 0, TINV = 2, P = TINV + NX * FT, TTURN = P + NO * FT, PTURN = TTURN + NX * FT;
+    static constexpr int key_units(bool save) { return (save ? 4 : 3) * NI * FK; }
+    static constexpr int value_units(bool save) { return save ? PTURN + NX * FT : TTURN; }
+    // unit of row tile i, step s (of piece 0; piece p is p * FK or p * FT further)
+    static constexpr __host__ __device__ int row(int i, int s) { return i * KS + s; }
+    static constexpr __host__ __device__ int turned(int i, int s) { return i * CS + s; }
+    static constexpr __host__ __device__ int lower(int i, int s) { return CS == 1 || i < 2 ? i : 2 * i - 2 + s; }
+    static constexpr __host__ __device__ int upper(int i, int s) { return CS == 1 ? i : i < 2 ? 2 * i + s : 2 + i; }
+};
+
+// a unit's operand: N pieces, `apart` units from one to the next
+template <int N>
+__device__ __forceinline__ Frag<N> unit(const char *base, int u, int apart)
 {
-    return (c & ~31) + 8 * ((c & 15) >> 2) + 4 * ((c & 31) >> 4) + (c & 3);
+    Frag<N> f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        f.p[i] = *reinterpret_cast<const bf16x8 *>(base + (u + i * apart) * UNIT + (threadIdx.x & 63) * 16);
+    return f;
+}
+template <int N>
+__device__ __forceinline__ void put_unit(char *base, int u, int apart, f32x8 x)
+{
+    const Frag<N> f = split<N>(x);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        *reinterpret_cast<bf16x8 *>(base + (int64_t)(u + i * apart) * UNIT + (threadIdx.x & 63) * 16) = f.p[i];
 }
 
-// N planes of ROWS x COLS bf16 pieces; 8 elements of padding spread the rows over the banks
-template <int N, int ROWS, int COLS>
-struct Planes {
-    static constexpr int LD = COLS + 8;
-    bf16_t e[N][ROWS][LD];
-    // the operand of rows r0 .. r0 + 15, summed elements 32 s .. 32 s + 31
-    __device__ __forceinline__ Frag<N> frag(int r0, int s) const
-    {
-        const int lane = threadIdx.x & 63;
-        Frag<N> f;
+// N units (up to 4) from memory to LDS by one wavefront: a lane's 16 bytes of a unit from `src` (uniform) + 16 lane to LDS address `at` (uniform) + 16 lane.
+// Written as assembly because the compiler waits for all loads in flight before it reads any LDS when it knows of one that writes there: who calls this
+// waits by wait_loads.  An instruction's offset counts for both addresses.  (The wait states are what a scalar register that a vector instruction has written,
+// as the address may be, has to have before a load takes it.)  The warning is about any clobber of m0; without it the compiler takes m0 for unchanged.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+template <int N>
+__device__ __forceinline__ void stream_units(const char *src, uint32_t at)
+{
+    const uint32_t off = (threadIdx.x & 63) * 16;
+    static_assert(N >= 1 && N <= 4 && UNIT == 1024, "offsets below 4096");
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(src) : "m0", "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(at), "v"(off),
+                     "s"(src)
+                     : "m0", "memory");
+    else if constexpr (N == 3)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:2048" ::"s"(at), "v"(off), "s"(src)
+                     : "m0", "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(at), "v"(off), "s"(src)
+                     : "m0", "memory");
+}
+#pragma clang diagnostic pop
+// A run of units by NW wavefronts, each its part of share(): the last ones' parts overlap where NW does not divide the run, so that all issue as many loads.
+template <int UNITS, int NW>
+constexpr int share()
+{
+    return (UNITS + NW - 1) / NW;
+}
+template <int UNITS, int NW>
+__device__ __forceinline__ void stream_run(const char *src, uint32_t at, int wave)
+{
+    constexpr int EACH = share<UNITS, NW>();
+    const int u = wave * EACH < UNITS - EACH ? wave * EACH : UNITS - EACH;
+    src += u * UNIT;
+    at += u * UNIT;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            f.p[i] = *reinterpret_cast<const bf16x8 *>(&e[i][r0 + (lane & 15)][32 * s + 8 * (lane >> 4)]);
-        return f;
-    }
-    // four elements c .. c + 3 of row r, c a multiple of four
-    __device__ __forceinline__ void put4(int r, int c, f32x4 x)
-    {
-        const int at = slot_of(c);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const bf16x4 h = __builtin_convertvector(x, bf16x4);
-            *reinterpret_cast<bf16x4 *>(&e[i][r][at]) = h;
-            if (i + 1 < N)
-                x -= __builtin_convertvector(h, f32x4);
-        }
-    }
-    __device__ __forceinline__ f32x4 get4(int r, int c) const
-    {
-        const int at = slot_of(c);
-        f32x4 x = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = N - 1; i >= 0; --i)
-            x += __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(&e[i][r][at]), f32x4);
-        return x;
-    }
-};
+    for (int i = 0; i + 4 <= EACH; i += 4)
+        stream_units<4>(src + i * UNIT, at + i * UNIT);
+    if constexpr (EACH % 4 != 0)
+        stream_units<EACH % 4>(src + EACH / 4 * 4 * UNIT, at + EACH / 4 * 4 * UNIT);
+}
+// the LDS address of a shared array
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
+// the sum over the 16 lanes of a row of lanes, in all of them
+__device__ __forceinline__ float row16_sum(float x)
+{
+#define LA_ROR(n) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xf, 0xf, false))
+    LA_ROR(8);
+    LA_ROR(4);
+    LA_ROR(2);
+    LA_ROR(1);
+#undef LA_ROR
+    return x;
+}
+// until at most N of this wavefront's loads (and stores) are in flight
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// A barrier that leaves loads and stores of memory in flight; this wavefront's reads of LDS are done.
+__device__ __forceinline__ void block_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // 8 elements of a row, those past `n` zero
 template <typename T>
@@ -147,31 +233,74 @@ __device__ __forceinline__ f32x8 load8(const T *p, int n)
     return f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
 }
 
-// A chunk of q or k: C rows of DKP elements (zeros past `len` rows and `dk` elements), as rows, and turned, summed over the tokens.
-template <typename T, int NI, int C, int DKP, bool ROWS, bool TURNED>
-__device__ __forceinline__ void stage_chunk(const T *src, int64_t ld, int len, int dk, Planes<NI, C, DKP> *rows, Planes<NI, DKP, C> *turned)
-{
-    constexpr int UC = DKP / 8, UNITS = (C / 4) * UC;
-    for (int u = threadIdx.x; u < UNITS; u += blockDim.x) {
-        const int c = 8 * (u % UC), r = 4 * (u / UC);
-        f32x8 x[4];
+// The walks' rows of v, o and their like pass through LDS, 16 bytes a lane: a wavefront that is alone on its SIMD pays for every instruction, and an access
+// of 2 bytes is one as well.  Rows past `rows` and columns past `cols` are not touched; nothing has to be aligned.
+// In: 16 NW columns of C rows, by all wavefronts; a chunk ahead into registers, then into LDS.
+template <typename T, int C, int NW>
+struct RowsIn {
+    static constexpr int PE = 16 / sizeof(T), RP = 16 * NW / PE, PER = C * RP / (64 * NW);  // elements of a pack, packs of a row, of a lane
+    using Pack16 = PackOf<T, 16 / sizeof(T)>;
+    typename Pack16::whole x[PER];
+    __device__ __forceinline__ void fetch(const T *src, int64_t ld, int rows, int cols)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x[i] = load8<T>(src + (int64_t)(r + i) * ld + c, r + i < len ? dk - c : 0);
-        if constexpr (ROWS) {
+        for (int k = 0; k < PER; ++k) {
+            const int u = k * 64 * NW + threadIdx.x, row = u / RP, c = u % RP * PE;
+            const T *at = src + row * ld + c;
+            if (row < rows && c + PE <= cols) {
+                x[k] = *(typename Pack16::source)at;
+            } else {
+                at = opaque(at);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                rows->put4(r + i, c, __builtin_shufflevector(x[i], x[i], 0, 1, 2, 3));
-                rows->put4(r + i, c + 4, __builtin_shufflevector(x[i], x[i], 4, 5, 6, 7));
+                for (int e = 0; e < PE; ++e)
+                    x[k][e] = row < rows && c + e < cols ? in_memory(at)[e] : (T)0.0f;
             }
         }
-        if constexpr (TURNED) {
+    }
+    __device__ __forceinline__ void put(char *lds) const
+    {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                turned->put4(c + j, r, f32x4{x[0][j], x[1][j], x[2][j], x[3][j]});
+        for (int k = 0; k < PER; ++k)
+            *reinterpret_cast<typename Pack16::whole *>(lds + (k * 64 * NW + threadIdx.x) * 16) = x[k];
+    }
+    static __device__ __forceinline__ float at(const char *lds, int row, int col) { return (float)*reinterpret_cast<const T *>(lds + (row * 16 * NW + col) * sizeof(T)); }
+};
+// Out: a wavefront's own 16 columns, C rows of an accumulator.
+template <typename T, int C>
+struct RowsOut {
+    static constexpr int ROW = 16 * sizeof(T) + 16, PE = 16 / sizeof(T), RP = sizeof(T);  // bytes of a row with its padding; elements of a pack, packs of a row
+    using Pack16 = PackOf<T, 16 / sizeof(T)>;
+    using whole = typename Pack16::whole;
+    static __device__ __forceinline__ void store(char *buf, T *dst, int64_t ld, const f32x4 *x, int rows, int cols)
+    {
+        const int lane = threadIdx.x & 63, col = lane & 15;
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < C / 16; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<T *>(buf + (first_of(i) + r) * ROW + col * sizeof(T)) = (T)x[i][r];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        whole y[C * RP / 64];
+#pragma unroll
+        for (int k = 0; k < C * RP / 64; ++k)
+            y[k] = *reinterpret_cast<const whole *>(buf + (k * (64 / RP) + lane / RP) * ROW + lane % RP * 16);
+#pragma unroll
+        for (int k = 0; k < C * RP / 64; ++k) {
+            const int row = k * (64 / RP) + lane / RP, c = lane % RP * PE;
+            T *at = dst + row * ld + c;
+            if (row < rows && c + PE <= cols) {
+                *(typename Pack16::target)at = y[k];
+            } else {
+                at = opaque(at);
+#pragma unroll
+                for (int e = 0; e < PE; ++e)
+                    if (row < rows && c + e < cols)
+                        in_memory(at)[e] = y[k][e];
+            }
         }
     }
-}
+};
 
 // a sequence's first token and length; what `offsets` holds is kept inside the tokens there are
 __device__ __forceinline__ void sequence(const DeltaArgs &p, int64_t n, int64_t &t0, int64_t &len)
@@ -224,38 +353,49 @@ __device__ __forceinline__ bool slot_chunk(const DeltaArgs &p, int64_t slot, int
     return true;
 }
 
-// Decays of a chunk: b_i the sum of g up to token i in 64 bits (differences of it are exact enough for any decay; g below -1000 counts as -1000, whose
-// exponential is zero), and what the products take from it.  Tokens past the end have g = beta = 0.
+// 2^x for x <= 0 in 64 bits: the whole part by the exponent, so that a large x costs no precision
+__device__ __forceinline__ float exp2_of(double x)
+{
+    const double n = rint(x);
+    return ldexpf(__builtin_amdgcn_exp2f((float)(x - n)), (int)fmax(n, -1000.0));
+}
+
+// Decays of a chunk: b_i the sum of g log2(e) up to token i in 64 bits (differences of it are exact enough for any decay; g below -1000 counts as -1000, whose
+// exponential is zero), and what the products take from it.  Tokens past the end have g = beta = 0.  The second unit is what the walks read.
 template <int C>
 struct alignas(16) Decays {
     double b[C];
-    float in[C], out[C], beta[C];  // exp(b_i), exp(b_last - b_i)
-    float all;                     // exp(b_last)
+    char rest[UNIT - 8 * C];
+    float in[C], out[C], beta[C];  // 2^b_i, 2^(b_last - b_i)
+    float all;                     // 2^b_last
+    char rest2[UNIT - (3 * C + 1) * 4];
     // by the lanes of one wavefront
     __device__ __forceinline__ void load(const float *g, const float *be, int64_t ld, int len)
     {
         const int i = threadIdx.x & 63;
-        double x = i < len ? fmax((double)g[(int64_t)i * ld], -1000.0) : 0.0;
-        if (i < len && g[(int64_t)i * ld] != g[(int64_t)i * ld])
-            x = g[(int64_t)i * ld];
+        float y = i < len ? g[(int64_t)i * ld] : 0.0f;
+        const float gate = i < len ? be[(int64_t)i * ld] : 0.0f;
+        y = y < -1000.0f ? -1000.0f : y;
+        double x = 1.4426950408889634074 * y;  // log2(e)
 #pragma unroll
         for (int s = 1; s < C; s *= 2) {
-            const double y = __shfl_up(x, s, 64);
+            const double z = __shfl_up(x, s, 64);
             if (i >= s)
-                x += y;
+                x += z;
         }
         const double last = __shfl(x, C - 1, 64);
         if (i < C) {
             b[i] = x;
-            in[i] = expf((float)x);
-            out[i] = expf((float)(last - x));
-            beta[i] = i < len ? be[(int64_t)i * ld] : 0.0f;
+            in[i] = exp2_of(x);
+            out[i] = exp2_of(last - x);
+            beta[i] = gate;
         }
         if (i == 0)
-            all = expf((float)last);
+            all = exp2_of(last);
     }
-    __device__ __forceinline__ float between(int i, int j) const { return expf((float)(b[i] - b[j])); }
-    __device__ __forceinline__ f32x4 four(const float *x, int i) const { return *reinterpret_cast<const f32x4 *>(x + i); }
+    __device__ __forceinline__ float between(int i, int j) const { return __builtin_amdgcn_exp2f((float)(b[i] - b[j])); }
+    static __device__ __forceinline__ f32x4 four(const float *x, int i) { return *reinterpret_cast<const f32x4 *>(x + i); }
 };
+static_assert(sizeof(Decays<64>) == 2 * UNIT && sizeof(Decays<32>) == 2 * UNIT, "two units");
 
 }  // namespace la

@@ -19,384 +19,516 @@
 
 namespace la {
 
+// Two halves a chunk as in the forward walk: K, P^T and the decays, then Q^T, K^T and T^T.
 template <typename T, int DKP, int NW>
 __global__ __launch_bounds__(64 * NW) void k_delta_scan_back(DeltaArgs p)
 {
-    constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI, RT = C / 16, KT = DKP / 16;
-    struct Tiles {
-        Planes<NI, C, DKP> K, Q;
-        Planes<NI, DKP, C> Kt, Qt;
-        Planes<NX, C, C> inv, P;  // T^T and P^T
-        Decays<C> d;
-    };
-    __shared__ __align__(16) Tiles m;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, row4 = 4 * (lane >> 4);
+    using G = Pack<T, DKP>;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, KT = G::KT;
+    constexpr int LD = NI * G::FK, LP = LD + 1, FIRST = LP + NX * G::FT;
+    constexpr int LQ = NI * G::FK, LT = 2 * NI * G::FK, SECOND = LT + NX * G::FT;  // second half: Kt, Qt, T^T
+    constexpr int EACH1 = share<LD, NW>() + 1 + share<FIRST - LP, NW>();
+    using In = RowsIn<T, C, NW>;
+    __shared__ __align__(16) char first[2][FIRST * UNIT];
+    __shared__ __align__(16) char second[SECOND * UNIT];
+    __shared__ __align__(16) char oin[C * 16 * NW * sizeof(T)];
+    __shared__ __align__(16) char turn[NW][C * RowsOut<float, C>::ROW];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
     const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
     const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int c0 = (slice * NW + wave) * 16 + col;
-    const bool live = c0 < p.dv, kept = c0 < p.dvp;
+    const int cbase = (slice * NW + wave) * 16, c0 = cbase + col;
+    const bool live = c0 < p.dv, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
     const int hk = h / (p.hv / p.hk);
-    const int64_t state_at = (n * p.hv + h) * p.dk * (int64_t)p.dv;
+    const int64_t state_at = (n * p.hv + h) * p.dk * (int64_t)p.dv, ldo = (int64_t)p.hv * p.dv;
+    const int64_t slot0 = first_slot<C>(p, n, t0);
+    const int chunks = (int)((len + C - 1) / C);
+    const int64_t key_step = (int64_t)p.hk * (G::key_units(true) * UNIT), value_step = (int64_t)p.hv * (G::value_units(true) * UNIT);
+    const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(true) * UNIT) + (chunks - 1) * key_step,
+               *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(true) * UNIT) + (chunks - 1) * value_step;
+    const uint32_t first_at = lds_address(first), second_at = lds_address(second);
+    auto fetch_first = [&](const char *k, const char *v, int buffer) {
+        const uint32_t at = first_at + buffer * (FIRST * UNIT);
+        stream_run<LD, NW>(k, at, wave);
+        stream_units<1>(v + UNIT, at + LD * UNIT);  // (the decays: by every wavefront)
+        stream_run<FIRST - LP, NW>(v + G::PTURN * UNIT, at + LP * UNIT, wave);
+    };
+    auto fetch_second = [&](const char *k, const char *v) {
+        stream_run<LT, NW>(k + G::KTURN * UNIT, second_at, wave);
+        stream_run<SECOND - LT, NW>(v + G::TTURN * UNIT, second_at + LT * UNIT, wave);
+    };
+    char *mine = turn[wave];
+    In O;
+    auto fetch_o = [&](int c) {
+        O.fetch((const T *)p.o_bar + ((t0 + (int64_t)c * C) * p.hv + h) * p.dv + slice * NW * 16, ldo, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                p.dv - slice * NW * 16);
+    };
+    auto keep_state = [&](int c, const f32x4 *S) {
+        if (kept) {
+            float *dst = p.chunk_state_bar + ((slot0 + c) * p.hv + h) * DKP * (int64_t)p.dvp + cbase;
+#pragma unroll
+            for (int i = 0; i < KT / RT; ++i)
+                RowsOut<float, C>::store(mine, dst + (int64_t)i * C * p.dvp, p.dvp, S + i * RT, C, 16);
+        }
+    };
 
     f32x4 S[KT];  // the gradient of the state after the chunk
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 16 * t + row4 + r;
+            const int i = first_of(t) + r;
             S[t][r] = p.state1_bar && live && i < p.dk ? p.state1_bar[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
-    for (int i = threadIdx.x; i < C * Planes<NX, C, C>::LD; i += 64 * NW)
-        for (int x = 0; x < NX; ++x)
-            (&m.P.e[x][0][0])[i] = (bf16_t)0.0f;
-
-    const int64_t chunks = (len + C - 1) / C;
-    int64_t slot = first_slot<C>(p, n, t0) + chunks - 1;
-    for (int64_t c = chunks - 1; c >= 0; --c, --slot) {
-        const int64_t t = t0 + c * C;
-        const int left = (int)(len - c * C < C ? len - c * C : C);
-        const int64_t sh = slot * p.hv + h;
-        __syncthreads();
-        stage_chunk<T, NI, C, DKP, true, true>((const T *)p.k + t * p.ldk + (int64_t)hk * p.dk, p.ldk, left, p.dk, &m.K, &m.Kt);
-        stage_chunk<T, NI, C, DKP, true, true>((const T *)p.q + t * p.ldq + (int64_t)hk * p.dk, p.ldq, left, p.dk, &m.Q, &m.Qt);
-        const float *inv = p.inv + sh * C * C;
-        for (int u = threadIdx.x; u < C * C / 16; u += 64 * NW) {
-            const int i = 4 * (u / (C / 4)), j = 4 * (u % (C / 4));
-            f32x4 x[4];
+    if (chunks > 0) {
+        fetch_first(pk, pv, (chunks - 1) & 1);
+        fetch_o(chunks - 1);
+        keep_state(chunks - 1, S);
+        O.put(oin);
+        wait_loads<0>();
+    }
+    for (int c = chunks - 1; c >= 0; --c, pk -= key_step, pv -= value_step) {
+        const char *a = first[c & 1];
+        block_barrier();
+        f32x4 Ob[RT], Y[RT], Z[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                x[r] = *reinterpret_cast<const f32x4 *>(inv + (i + r) * C + j);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                m.inv.put4(j + r, i, f32x4{x[0][r], x[1][r], x[2][r], x[3][r]});
-        }
-        if (wave == 0)
-            m.d.load(p.g + t * p.hv + h, p.beta + t * p.hv + h, p.hv, left);
-        f32x4 O[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + row4 + r;
-                O[i][r] = live && row < left ? (float)((const T *)p.o_bar)[((t + row) * p.hv + h) * p.dv + c0] : 0.0f;
-            }
-        __syncthreads();
-        // P^T: lane's column is the key, its four rows the queries
-        for (int j = wave; j < RT; j += NW)
-            for (int i = j; i < RT; ++i) {
-                f32x4 x = {0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < DKP / 32; ++s)
-                    mma(x, m.Q.frag(16 * i, s), m.K.frag(16 * j, s));
-                const int kj = 16 * j + col;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int qi = 16 * i + row4 + r;
-                    x[r] = kj <= qi ? p.scale * m.d.between(qi, kj) * x[r] : 0.0f;
-                }
-                m.P.put4(kj, 16 * i + row4, x);
-            }
-        if (kept) {
-            float *out = p.chunk_state_bar + sh * DKP * (int64_t)p.dvp + c0;
-#pragma unroll
-            for (int i = 0; i < KT; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    out[(int64_t)(16 * i + row4 + r) * p.dvp] = S[i][r];
-        }
-        f32x4 Y[RT], Z[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
+                Ob[i][r] = In::at(oin, first_of(i) + r, 16 * wave + col);
             Y[i] = Z[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < DKP / 32; ++s) {
-            const Frag<NX> f = split<NX>(join(S[2 * s], S[2 * s + 1]));
+        }
+        Frag<NI> kf[2][RT];
+        Frag<NX> pf[G::FT];
+        auto rows_of = [&](int s, Frag<NI> *k) {
 #pragma unroll
             for (int i = 0; i < RT; ++i)
-                mma(Y[i], m.K.frag(16 * i, s), f);
+                k[i] = unit<NI>(a, G::row(i, s), G::FK);
+        };
+        rows_of(0, kf[0]);
+        issue_point();
+        fetch_second(pk, pv);
+        if (c > 0)
+            fetch_first(pk - key_step, pv - value_step, ~c & 1);
+        Frag<NX> f = split<NX>(join(S[0], S[1]));
+#pragma unroll
+        for (int s = 0; s < G::KS; ++s) {
+            if (s + 1 < G::KS) {
+                rows_of(s + 1, kf[~s & 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < G::FT; ++i)
+                    pf[i] = unit<NX>(a, LP + i, G::FT);
+            }
+            issue_point();
+            const Frag<NX> now = f;
+            if (s + 1 < G::KS)
+                f = split<NX>(join(S[2 * s + 2], S[2 * s + 3]));
+            mma_tiles<3, RT>(Y, kf[s & 1], now);
+        }
+        const Decays<C> &d = *reinterpret_cast<const Decays<C> *>(a + (LD - 1) * UNIT);  // (its second unit)
+        f32x4 in[RT], beta[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            Y[i] *= d.four(d.out, first_of(i));
+            in[i] = d.four(d.in, first_of(i));
+            beta[i] = d.four(d.beta, first_of(i));
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            Y[i] *= m.d.four(m.d.out, 16 * i + row4);
-        __syncthreads();  // P^T is there
-        const float all = m.d.all;
+        for (int s = 0; s < G::CS; ++s) {
+            const Frag<NI> o = split<NI>(join(Ob[2 * s], Ob[2 * s + 1]));
+#pragma unroll
+            for (int j = 0; j < 2 * s + 2; ++j)
+                mma<3>(Y[j], pf[G::upper(j, s)], o);
+        }
+        const float all = d.all;
 #pragma unroll
         for (int i = 0; i < KT; ++i)
             S[i] *= all;
-#pragma unroll
-        for (int s = 0; s < C / 32; ++s) {
-            const Frag<NI> f = split<NI>(join(O[2 * s], O[2 * s + 1]));
-#pragma unroll
-            for (int j = 0; j < 2 * s + 2; ++j)
-                mma(Y[j], m.P.frag(16 * j, s), f);
-            const Frag<NX> w = split<NX>(join(O[2 * s] * p.scale * m.d.four(m.d.in, 32 * s + row4), O[2 * s + 1] * p.scale * m.d.four(m.d.in, 32 * s + 16 + row4)));
+        if (c > 0)
+            wait_loads<EACH1>();
+        else
+            wait_loads<0>();
+        block_barrier();
+        if (c > 0)
+            fetch_o(c - 1);
+        Frag<NX> tf[G::FT];
+        Frag<NI> ktf[2][KT];
+        auto turned_of = [&](int from, int s, Frag<NI> *k) {
 #pragma unroll
             for (int i = 0; i < KT; ++i)
-                mma(S[i], m.Qt.frag(16 * i, s), w);
-        }
+                k[i] = unit<NI>(second, from + G::turned(i, s), G::FK);
+        };
 #pragma unroll
-        for (int s = 0; s < C / 32; ++s) {
-            const Frag<NX> f = split<NX>(join(Y[2 * s], Y[2 * s + 1]));
+        for (int i = 0; i < G::FT; ++i)
+            tf[i] = unit<NX>(second, LT + i, G::FT);
+        turned_of(LQ, 0, ktf[0]);
+        issue_point();
+#pragma unroll
+        for (int s = 0; s < G::CS; ++s) {  // Q^T scale exp(b) O_bar, and Z
+            turned_of(s + 1 < G::CS ? LQ : 0, s + 1 < G::CS ? s + 1 : 0, ktf[~s & 1]);
+            issue_point();
+            const Frag<NX> y = split<NX>(join(Y[2 * s], Y[2 * s + 1]));
 #pragma unroll
             for (int j = 0; j < 2 * s + 2; ++j)
-                mma(Z[j], m.inv.frag(16 * j, s), f);
+                mma<3>(Z[j], tf[G::upper(j, s)], y);
+            mma_tiles<3, KT>(S, ktf[s & 1], split<NX>(join(Ob[2 * s] * (p.scale * in[2 * s]), Ob[2 * s + 1] * (p.scale * in[2 * s + 1]))));
         }
-        if (kept) {
-            float *out = p.chunk_z_bar + sh * C * (int64_t)p.dvp + c0;
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    out[(int64_t)(16 * i + row4 + r) * p.dvp] = Z[i][r];
-        }
+        f32x4 Vb[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i)
-            Z[i] *= m.d.four(m.d.beta, 16 * i + row4);
-        if (live) {
+            Vb[i] = Z[i] * beta[i];
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * i + row4 + r;
-                    if (row < left)
-                        ((T *)p.v_bar)[((t + row) * p.hv + h) * p.dv + c0] = (T)Z[i][r];
-                }
+        for (int s = 0; s < G::CS; ++s) {
+            if (s + 1 < G::CS) {
+                turned_of(0, s + 1, ktf[(G::CS + s + 1) & 1]);
+                issue_point();
+            }
+            mma_tiles<3, KT>(S, ktf[(G::CS + s) & 1], split<NX>(join(-Vb[2 * s] * in[2 * s], -Vb[2 * s + 1] * in[2 * s + 1])));
         }
-#pragma unroll
-        for (int s = 0; s < C / 32; ++s) {
-            const Frag<NX> w = split<NX>(join(-Z[2 * s] * m.d.four(m.d.in, 32 * s + row4), -Z[2 * s + 1] * m.d.four(m.d.in, 32 * s + 16 + row4)));
-#pragma unroll
-            for (int i = 0; i < KT; ++i)
-                mma(S[i], m.Kt.frag(16 * i, s), w);
-        }
+        wait_loads<0>();  // (before the stores: the next chunk does not wait for them)
+        if (c > 0)
+            O.put(oin);
+        const int64_t t = t0 + (int64_t)c * C;
+        const int left = (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C);
+        RowsOut<T, C>::store(mine, (T *)p.v_bar + (t * p.hv + h) * p.dv + cbase, ldo, Vb, left, p.dv - cbase);
+        if (kept)
+            RowsOut<float, C>::store(mine, p.chunk_z_bar + ((slot0 + c) * p.hv + h) * C * (int64_t)p.dvp + cbase, p.dvp, Z, C, 16);
+        if (c > 0)
+            keep_state(c - 1, S);
     }
     if (p.state0_bar && live) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + row4 + r;
+                const int i = first_of(t) + r;
                 if (i < p.dk)
                     p.state0_bar[state_at + (int64_t)i * p.dv + c0] = S[t][r];
             }
     }
 }
 
-// One block a chunk and key head.  A wavefront owns DKP / 4 columns of Q_bar and K_bar over all tokens of the chunk, and the 16 rows `wave` of M and N.
+// One block a chunk and key head, a wavefront for each 16 columns of Q_bar and K_bar over all tokens of the chunk.  The products summed over dv take 32
+// columns of O_bar, Z_bar and U at a time, through LDS, while the next 32 are loaded: once for M and N, once for the products with the states (all at once do
+// not fit the registers, and what does not fit waits for memory at every access).  M and N are formed as operands in both directions, by
+// exchanging the factors: their tiles go to LDS in units, split once, not by every wavefront that reads them.
 template <typename T, int DKP>
-__global__ __launch_bounds__(256) void k_delta_grads(DeltaArgs p)
+__global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 {
-    constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI, RT = C / 16, CT = DKP / 64;
-    struct Tiles {
-        Planes<NI, DKP, C> Kt, Qt;
-        Planes<NI, C, 32> O;     // 32 columns of O_bar, Z_bar, U at a time
-        Planes<NX, C, 32> Z, U;
-        float M[C][C + 4], N[C][C + 4];
-        Decays<C> d;
-        float dots[4][4][C];  // by wavefront: q.Q_bar, k.K_bar, k.H; last: k.(exp(b_last - b) U S1_bar^T)
-        float zv[C];
-        double states[4];
-    };
-    __shared__ __align__(16) Tiles m;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, row4 = 4 * (lane >> 4);
+    using G = Pack<T, DKP>;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FT = G::FT, NW = DKP / 16, NT = 64 * NW;
+    constexpr int LZ = NI * RT, LU = LZ + NX * RT, STAGE = LU + NX * RT;  // units of 32 columns
+    constexpr int JM = 0, JN = NX * FT, JMT = 2 * NX * FT, JNT = 3 * NX * FT;  // units of M, N and turned M, beta N
+    constexpr bool BOTH = 2 * RT > NW;  // a wavefront forms a row and column tile of M and of N, else of one of them
+    __shared__ __align__(16) char stage[2][STAGE * UNIT];
+    __shared__ __align__(16) char joint[4 * NX * FT * UNIT];
+    __shared__ Decays<C> d;
+    __shared__ __align__(16) float dots[4][NW][C];  // by wavefront: q.Q_bar, k.K_bar, k.H; last: k.(exp(b_last - b) U S1_bar^T)
+    __shared__ float zv_box[C];
+    __shared__ double state_box[NW];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15, x4 = lane >> 4;
     const int hk = blockIdx.x % p.hk, group = p.hv / p.hk;
     const int64_t slot = blockIdx.x / p.hk;
     if (p.offsets) {  // tokens of no sequence: zeros
         const int64_t a = p.offsets[0], z = p.offsets[p.batch];
         for (int64_t t = slot * C; t < (slot + 1) * C && t < p.tokens; ++t)
             if (t < a || t >= z) {
-                for (int c = threadIdx.x; c < p.dk; c += 256) {
+                for (int c = threadIdx.x; c < p.dk; c += NT) {
                     ((T *)p.q_bar)[(t * p.hk + hk) * p.dk + c] = (T)0.0f;
                     ((T *)p.k_bar)[(t * p.hk + hk) * p.dk + c] = (T)0.0f;
                 }
-                for (int h = hk * group; h < (hk + 1) * group; ++h) {
-                    for (int c = threadIdx.x; c < p.dv; c += 256)
-                        ((T *)p.v_bar)[(t * p.hv + h) * p.dv + c] = (T)0.0f;
-                    if (threadIdx.x == 0)
-                        p.g_bar[t * p.hv + h] = p.beta_bar[t * p.hv + h] = 0.0f;
-                }
+                for (int c = threadIdx.x; c < group * p.dv; c += NT)
+                    ((T *)p.v_bar)[(t * p.hv + hk * group) * p.dv + c] = (T)0.0f;
+                for (int c = threadIdx.x; c < group; c += NT)
+                    p.g_bar[t * p.hv + hk * group + c] = p.beta_bar[t * p.hv + hk * group + c] = 0.0f;
             }
     }
     int64_t t0;
     int len;
     if (!slot_chunk<C>(p, slot, t0, len))
         return;
-    stage_chunk<T, NI, C, DKP, false, true>((const T *)p.k + t0 * p.ldk + (int64_t)hk * p.dk, p.ldk, len, p.dk, (Planes<NI, C, DKP> *)nullptr, &m.Kt);
-    stage_chunk<T, NI, C, DKP, false, true>((const T *)p.q + t0 * p.ldq + (int64_t)hk * p.dk, p.ldq, len, p.dk, (Planes<NI, C, DKP> *)nullptr, &m.Qt);
-    f32x4 Qs[RT][CT], Ks[RT][CT];
+    const char *pk = p.pack_k + (slot * p.hk + hk) * (int64_t)(G::key_units(true) * UNIT);
+    // the four tokens of tile i that this lane's accumulators hold, of this lane's column of k or q
+    auto four_of = [&](const Frag<NI> *f, int i) {
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = NI - 1; k >= 0; --k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                x[r] += (float)f[i >> 1].p[k][4 * (i & 1) + r];
+        return x;
+    };
+    f32x4 Qs[RT], Ks[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-            Qs[i][c] = Ks[i][c] = f32x4{0, 0, 0, 0};
-    const int k0 = wave * 16 * CT;  // this wavefront's columns
+        Qs[i] = Ks[i] = f32x4{0, 0, 0, 0};
+    const int kcol = element_of(wave, col);  // this lane's column
+    const bool form_m = BOTH || wave < RT, form_n = BOTH || (wave >= RT && wave < 2 * RT);
+    const int tile = wave % RT;
 
     for (int h = hk * group; h < (hk + 1) * group; ++h) {
         const int64_t sh = slot * p.hv + h;
-        const float *S0 = p.chunk_state + sh * DKP * (int64_t)p.dvp, *S1 = p.chunk_state_bar + sh * DKP * (int64_t)p.dvp;
+        const float *S0 = p.chunk_state + sh * DKP * (int64_t)p.dvp + 8 * x4;
+        const float *S1 = p.chunk_state_bar + sh * DKP * (int64_t)p.dvp + 8 * x4;
         const float *Ug = p.chunk_u + sh * C * (int64_t)p.dvp, *Zg = p.chunk_z_bar + sh * C * (int64_t)p.dvp;
-        if (wave == 0)
-            m.d.load(p.g + t0 * p.hv + h, p.beta + t0 * p.hv + h, p.hv, len);
-        f32x4 a1[RT][CT], a2[RT][CT], a3[RT][CT], mp[RT], np[RT];
+        if (wave == 0) {
+            const char *pv = p.pack_v + sh * (int64_t)(G::value_units(true) * UNIT);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            mp[i] = np[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                a1[i][c] = a2[i][c] = a3[i][c] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<f32x4 *>((char *)&d + i * UNIT + 16 * lane) = *reinterpret_cast<const f32x4 *>(pv + i * UNIT + 16 * lane);
         }
-        float zv = 0;
-        double states = 0;
-        for (int s = 0; s < p.dvp / 32; ++s) {
-            __syncthreads();  // the columns before are read
-            if (threadIdx.x < 4 * C) {
-                const int r = threadIdx.x / 4, x = 8 * (threadIdx.x % 4), c = 32 * s + x;
-                const f32x8 o = load8<T>((const T *)p.o_bar + ((t0 + r) * p.hv + h) * p.dv + c, r < len ? p.dv - c : 0);
-                const f32x8 v = load8<T>((const T *)p.v + (t0 + r) * p.ldv + (int64_t)h * p.dv + c, r < len ? p.dv - c : 0);
-                const f32x8 z = load8<float>(Zg + (int64_t)r * p.dvp + c, 8), u = load8<float>(Ug + (int64_t)r * p.dvp + c, 8);
+        // row tile `tile` as columns of the accumulators (its rows the keys: M and N), column tile `tile` (its rows the queries: turned)
+        struct Pair {
+            f32x4 row[RT], turned[RT];
+        };
+        Pair pair[BOTH ? 2 : 1];  // of M, and of N in the last
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    zv += z[i] * v[i];
-                m.O.put4(r, x, __builtin_shufflevector(o, o, 0, 1, 2, 3));
-                m.O.put4(r, x + 4, __builtin_shufflevector(o, o, 4, 5, 6, 7));
-                m.Z.put4(r, x, __builtin_shufflevector(z, z, 0, 1, 2, 3));
-                m.Z.put4(r, x + 4, __builtin_shufflevector(z, z, 4, 5, 6, 7));
-                m.U.put4(r, x, __builtin_shufflevector(u, u, 0, 1, 2, 3));
-                m.U.put4(r, x + 4, __builtin_shufflevector(u, u, 4, 5, 6, 7));
+        for (int i = 0; i < RT; ++i)
+            for (Pair &x : pair)
+                x.row[i] = x.turned[i] = f32x4{0, 0, 0, 0};
+        float zv = 0, states = 0;
+        // 8 columns of a row: of Z_bar and V, or of O_bar and U
+        constexpr int ROUNDS = (8 * C + NT - 1) / NT;
+        f32x8 in0[ROUNDS], in1[ROUNDS];
+        auto fetch = [&](int s, bool with_v) {
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int u = threadIdx.x + k * NT;
+                const int r = u / 4 % C, c = 32 * s + 8 * (u % 4);
+                if (u < 4 * C) {
+                    in0[k] = load8<float>(Zg + r * p.dvp + c, 8);
+                    if (with_v)
+                        in1[k] = load8<T>((const T *)p.v + (t0 + r) * p.ldv + (int64_t)h * p.dv + c, r < len ? p.dv - c : 0);
+                } else if (u < 8 * C) {
+                    in0[k] = load8<T>((const T *)p.o_bar + ((t0 + r) * p.hv + h) * p.dv + c, r < len ? p.dv - c : 0);
+                    in1[k] = load8<float>(Ug + r * p.dvp + c, 8);
+                }
             }
-            Frag<NX> f0[CT], f1[CT];
+        };
+        auto put = [&](char *at, bool with_v) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const int64_t at = (int64_t)(k0 + 16 * c + col) * p.dvp + 32 * s + row4;
-                const f32x8 x = join(*reinterpret_cast<const f32x4 *>(S0 + at), *reinterpret_cast<const f32x4 *>(S0 + at + 16));
-                const f32x8 y = join(*reinterpret_cast<const f32x4 *>(S1 + at), *reinterpret_cast<const f32x4 *>(S1 + at + 16));
-                float sum = 0;
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int u = threadIdx.x + k * NT;
+                const int r = u / 4 % C;
+                // token r: row 4 (r / 8 % 4) + r % 4 of tile 2 (r / 32) + r / 4 % 2
+                const int t = 2 * (r >> 5) + ((r >> 2) & 1);
+                char *to = at + 16 * (16 * (u % 4) + 4 * ((r >> 3) & 3) + (r & 3));
+                if (u < 4 * C) {
+                    if (with_v) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    sum += x[i] * y[i];
-                states += sum;
-                f0[c] = split<NX>(x);
-                f1[c] = split<NX>(y);
+                        for (int i = 0; i < 8; ++i)
+                            zv += in0[k][i] * in1[k][i];
+                    }
+                    const Frag<NX> f = split<NX>(in0[k]);
+#pragma unroll
+                    for (int i = 0; i < NX; ++i)
+                        *reinterpret_cast<bf16x8 *>(to + (LZ + i * RT + t) * UNIT) = f.p[i];
+                } else if (u < 8 * C) {
+                    const Frag<NI> f = split<NI>(in0[k]);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+                        *reinterpret_cast<bf16x8 *>(to + (i * RT + t) * UNIT) = f.p[i];
+                    const Frag<NX> g = split<NX>(in1[k]);
+#pragma unroll
+                    for (int i = 0; i < NX; ++i)
+                        *reinterpret_cast<bf16x8 *>(to + (LU + i * RT + t) * UNIT) = g.p[i];
+                }
             }
+        };
+        const int steps = p.dvp / 32;
+        int turn = 0;
+        fetch(0, true);
+        for (int s = 0; s < steps; ++s, turn ^= 1) {
+            char *at = stage[turn];
+            put(at, true);
             __syncthreads();
+            if (s + 1 < steps)
+                fetch(s + 1, true);
+            // M, N: whether this wavefront forms them; HIGH: its tile is in the second half of the tokens
+            auto products = [&](auto M, auto N, auto HIGH) {
+                Frag<NI> ot;
+                Frag<NX> zt;
+                const Frag<NX> ut = unit<NX>(at, LU + tile, RT);
+                if constexpr (M.value)
+                    ot = unit<NI>(at, tile, RT);
+                if constexpr (N.value)
+                    zt = unit<NX>(at, LZ + tile, RT);
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                const Frag<NI> o = m.O.frag(16 * i, 0);
-                const Frag<NX> z = m.Z.frag(16 * i, 0), u = m.U.frag(16 * i, 0);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    mma(a1[i][c], o, f0[c]);
-                    mma(a2[i][c], z, f0[c]);
-                    mma(a3[i][c], u, f1[c]);
+                for (int i = 0; i < RT; ++i) {
+                    const Frag<NX> u = unit<NX>(at, LU + i, RT);
+                    const bool row = CS == 1 || HIGH.value || i < 2, turned = CS == 1 || !HIGH.value || i >= 2;
+                    if constexpr (M.value) {
+                        if (row)
+                            mma<3>(pair[0].row[i], u, ot);
+                        if (turned)
+                            mma<3>(pair[0].turned[i], unit<NI>(at, i, RT), ut);
+                    }
+                    if constexpr (N.value) {
+                        if (row)
+                            mma<3>(pair[BOTH].row[i], u, zt);
+                        if (turned)
+                            mma<3>(pair[BOTH].turned[i], unit<NX>(at, LZ + i, RT), ut);
+                    }
                 }
-                if (wave < RT && i <= wave) {  // rows `wave` of M and N, columns i
-                    mma(mp[i], m.O.frag(16 * wave, 0), u);
-                    mma(np[i], m.Z.frag(16 * wave, 0), u);
-                }
+            };
+            using Yes = std::true_type;
+            using No = std::false_type;
+            const bool high = CS > 1 && tile >= 2;
+            if constexpr (BOTH) {
+                if (high)
+                    products(Yes{}, Yes{}, Yes{});
+                else
+                    products(Yes{}, Yes{}, No{});
+            } else if (form_m) {
+                if (high)
+                    products(Yes{}, No{}, Yes{});
+                else
+                    products(Yes{}, No{}, No{});
+            } else if (form_n) {
+                if (high)
+                    products(No{}, Yes{}, Yes{});
+                else
+                    products(No{}, Yes{}, No{});
             }
         }
-        // M and N
-        if (wave < RT) {
-#pragma unroll
-            for (int j = 0; j < RT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int qi = 16 * wave + row4 + r, kj = 16 * j + col;
-                    const float e = kj <= qi ? m.d.between(qi, kj) : 0.0f;
-                    m.M[qi][kj] = kj <= qi ? p.scale * e * mp[j][r] : 0.0f;
-                    m.N[qi][kj] = kj < qi ? -e * np[j][r] : 0.0f;
-                }
-        }
+        f32x8 st0, st1;
+        auto fetch_states = [&](int s) {
+            st0 = load8<float>(S0 + kcol * p.dvp + 32 * s, 8);
+            st1 = load8<float>(S1 + kcol * p.dvp + 32 * s, 8);
+        };
+        fetch(0, false);
+        fetch_states(0);
         zv += __shfl_xor(zv, 1, 64);
         zv += __shfl_xor(zv, 2, 64);
         if (threadIdx.x < 4 * C && threadIdx.x % 4 == 0)
-            m.zv[threadIdx.x / 4] = zv;
-        states = wave_sum(states);
-        if (lane == 0)
-            m.states[wave] = states;
+            zv_box[threadIdx.x / 4] = zv;
+        // decays over M and N, and their units
+        const int mine = element_of(tile, col);  // this lane's token
+        f32x4 before[RT], after[RT];             // decays from token x to `mine`, from `mine` to x; zero where there is none
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const f32x4 in = m.d.four(m.d.in, 16 * i + row4), out = m.d.four(m.d.out, 16 * i + row4);
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                a1[i][c] *= p.scale * in;
-                a2[i][c] *= -in;
-                a3[i][c] *= out;
+            for (int r = 0; r < 4; ++r) {
+                const int x = first_of(i) + r;
+                before[i][r] = x <= mine ? d.between(mine, x) : 0.0f;
+                after[i][r] = mine <= x ? d.between(x, mine) : 0.0f;
             }
-        }
-        auto dots = [&](int which, auto &&a, const Planes<NI, DKP, C> &x) {
+        auto put_joint = [&](Pair &y, bool m) {  // row: query `mine`, keys x; turned: queries x, key `mine`
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                f32x4 d = {0, 0, 0, 0};
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int c = 0; c < CT; ++c)
-                    d += a[i][c] * x.get4(k0 + 16 * c + col, 16 * i + row4);
+                for (int r = 0; r < 4; ++r) {
+                    const int x = first_of(i) + r;
+                    const float e = before[i][r], f = after[i][r];
+                    y.row[i][r] = m ? (e != 0 ? p.scale * e * y.row[i][r] : 0.0f) : (e != 0 && x != mine ? -e * y.row[i][r] : 0.0f);
+                    y.turned[i][r] = m ? (f != 0 ? p.scale * f * y.turned[i][r] : 0.0f) : (f != 0 && x != mine ? -d.beta[x] * f * y.turned[i][r] : 0.0f);
+                }
 #pragma unroll
-                for (int k = 1; k < 16; k *= 2)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        d[r] += __shfl_xor(d[r], k, 64);
-                if (col == 0)
-                    *reinterpret_cast<f32x4 *>(&m.dots[which][wave][16 * i + row4]) = d;
+            for (int s = 0; s < CS; ++s) {
+                if (s <= tile / 2)
+                    put_unit<NX>(joint, (m ? JM : JN) + G::lower(tile, s), FT, join(y.row[2 * s], y.row[2 * s + 1]));
+                if (s >= tile / 2)
+                    put_unit<NX>(joint, (m ? JMT : JNT) + G::upper(tile, s), FT, join(y.turned[2 * s], y.turned[2 * s + 1]));
             }
         };
-        dots(3, a3, m.Kt);
-        __syncthreads();  // M and N are there
+        if (form_m)
+            put_joint(pair[0], true);
+        if (form_n)
+            put_joint(pair[BOTH], false);
+        f32x4 a1[RT], a2[RT], a3[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {  // rows i of the results
+        for (int i = 0; i < RT; ++i)
+            a1[i] = a2[i] = a3[i] = f32x4{0, 0, 0, 0};
+        for (int s = 0; s < steps; ++s, turn ^= 1) {
+            char *at = stage[turn];
+            put(at, false);
 #pragma unroll
-            for (int s = 0; s < C / 32; ++s) {
-                const int row = 16 * i + col, at = 32 * s + row4;
-                if (2 * s <= i) {
-                    const Frag<NX> fm = split<NX>(join(*reinterpret_cast<const f32x4 *>(&m.M[row][at]), *reinterpret_cast<const f32x4 *>(&m.M[row][at + 16])));
-                    const Frag<NX> fn = split<NX>(join(*reinterpret_cast<const f32x4 *>(&m.N[row][at]), *reinterpret_cast<const f32x4 *>(&m.N[row][at + 16])));
+            for (int i = 0; i < 8; ++i)
+                states += st0[i] * st1[i];
+            const Frag<NX> f0 = split<NX>(st0), f1 = split<NX>(st1);
+            __syncthreads();
+            if (s + 1 < steps) {
+                fetch(s + 1, false);
+                fetch_states(s + 1);
+            }
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) {
-                        const Frag<NI> k = m.Kt.frag(k0 + 16 * c, s);
-                        mma(a1[i][c], fm, k);
-                        mma(a2[i][c], fn, k);
-                    }
-                }
-                if (2 * s + 1 >= i) {
-                    f32x8 x, y;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const int t = at + (r & 3) + 16 * (r >> 2);
-                        x[r] = m.M[t][row];
-                        y[r] = m.d.beta[t] * m.N[t][row];
-                    }
-                    const Frag<NX> fm = split<NX>(x), fn = split<NX>(y);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) {
-                        mma(a3[i][c], fm, m.Qt.frag(k0 + 16 * c, s));
-                        mma(a3[i][c], fn, m.Kt.frag(k0 + 16 * c, s));
-                    }
-                }
+            for (int i = 0; i < RT; ++i) {
+                mma<3>(a2[i], unit<NX>(at, LZ + i, RT), f0);
+                mma<3>(a3[i], unit<NX>(at, LU + i, RT), f1);
+                mma<3>(a1[i], unit<NI>(at, i, RT), f0);
             }
         }
-        dots(2, a2, m.Kt);
+        Frag<NI> kt[CS], qt[CS];
+#pragma unroll
+        for (int s = 0; s < CS; ++s) {
+            kt[s] = unit<NI>(pk, G::KTURN + G::turned(wave, s), G::FK);
+            qt[s] = unit<NI>(pk, G::QTURN + G::turned(wave, s), G::FK);
+        }
+        const double sum = wave_sum((double)states);
+        if (lane == 0)
+            state_box[wave] = sum;
+        auto dot = [&](int which, const f32x4 (&a)[RT], const Frag<NI> (&f)[CS]) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                f32x4 x = a[i] * four_of(f, i);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[r] = row16_sum(x[r]);
+                if (col == 0)
+                    *reinterpret_cast<f32x4 *>(&dots[which][wave][first_of(i)]) = x;
+            }
+        };
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const f32x4 beta = m.d.four(m.d.beta, 16 * i + row4);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                a3[i][c] += beta * a2[i][c];
-                Qs[i][c] += a1[i][c];
-                Ks[i][c] += a3[i][c];
-            }
+            const f32x4 in = d.four(d.in, first_of(i));
+            a1[i] *= p.scale * in;
+            a2[i] *= -in;
+            a3[i] *= d.four(d.out, first_of(i));
         }
-        dots(0, a1, m.Qt);
-        dots(1, a3, m.Kt);
+        dot(3, a3, kt);
+#pragma unroll
+        for (int s = 0; s < CS; ++s)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {  // row tile i of the results
+                if (s <= i / 2) {
+                    const Frag<NX> mf = unit<NX>(joint, JM + G::lower(i, s), FT), nf = unit<NX>(joint, JN + G::lower(i, s), FT);
+                    mma<3>(a1[i], mf, kt[s]);
+                    mma<3>(a2[i], nf, kt[s]);
+                }
+                if (s >= i / 2) {
+                    const Frag<NX> mf = unit<NX>(joint, JMT + G::upper(i, s), FT), nf = unit<NX>(joint, JNT + G::upper(i, s), FT);
+                    mma<3>(a3[i], mf, qt[s]);
+                    mma<3>(a3[i], nf, kt[s]);
+                }
+            }
+        dot(2, a2, kt);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            a3[i] += d.four(d.beta, first_of(i)) * a2[i];
+            Qs[i] += a1[i];
+            Ks[i] += a3[i];
+        }
+        dot(0, a1, qt);
+        dot(1, a3, kt);
         __syncthreads();
         if (wave == 0) {
             const int i = lane < C ? lane : C - 1;
-            auto whole = [&](int which) { return (double)m.dots[which][0][i] + m.dots[which][1][i] + m.dots[which][2][i] + m.dots[which][3][i]; };
+            auto whole = [&](int which) {
+                double x = 0;
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+                    x += dots[which][w][i];
+                return x;
+            };
             const double kh = whole(2);
-            double last = lane < C ? whole(3) : 0.0;
-            last = wave_sum(last) + m.d.all * (m.states[0] + m.states[1] + m.states[2] + m.states[3]);
-            double x = lane < C ? whole(0) + 2.0 * m.d.beta[i] * kh - whole(1) : 0.0;
+            double last = lane < C ? whole(3) : 0.0, both = 0;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                both += state_box[w];
+            last = wave_sum(last) + d.all * both;
+            double x = lane < C ? whole(0) + 2.0 * d.beta[i] * kh - whole(1) : 0.0;
 #pragma unroll
             for (int s = 1; s < C; s *= 2) {  // from the chunk's end
                 const double y = __shfl_down(x, s, 64);
@@ -405,24 +537,22 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaArgs p)
             }
             if (lane < len) {
                 p.g_bar[(t0 + lane) * p.hv + h] = (float)(x + last);
-                p.beta_bar[(t0 + lane) * p.hv + h] = (float)(m.zv[i] + kh);
+                p.beta_bar[(t0 + lane) * p.hv + h] = (float)(zv_box[i] + kh);
             }
         }
-        __syncthreads();  // the next head overwrites the decays and dots
+        __syncthreads();  // the next head overwrites what this one reads
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + row4 + r, k = k0 + 16 * c + col;
-                if (row < len && k < p.dk) {
-                    const int64_t at = ((t0 + row) * p.hk + hk) * p.dk + k;
-                    ((T *)p.q_bar)[at] = (T)Qs[i][c][r];
-                    ((T *)p.k_bar)[at] = (T)Ks[i][c][r];
-                }
+        for (int r = 0; r < 4; ++r) {
+            const int row = first_of(i) + r;
+            if (row < len && kcol < p.dk) {
+                const int64_t at = ((t0 + row) * p.hk + hk) * p.dk + kcol;
+                in_memory((T *)p.q_bar)[at] = (T)Qs[i][r];
+                in_memory((T *)p.k_bar)[at] = (T)Ks[i][r];
             }
+        }
 }
 
 template <typename T, int DKP>
@@ -432,7 +562,7 @@ static la_status back_t(DeltaArgs &p, hipStream_t st)
     p.slices = (p.dv + 16 * NW - 1) / (16 * NW);
     LA_LAUNCH((k_delta_scan_back<T, DKP, NW>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(64 * NW), 0, st, p);
     if (p.slots > 0)
-        LA_LAUNCH((k_delta_grads<T, DKP>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
+        LA_LAUNCH((k_delta_grads<T, DKP>), dim3((unsigned)(p.slots * p.hk)), dim3(4 * DKP), 0, st, p);
     return launch_check("delta rule backward");
 }
 

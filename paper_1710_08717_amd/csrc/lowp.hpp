@@ -23,22 +23,28 @@ using acc_of = typename AccOf<T>::type;
 // vector loads and stores off their own alignment.
 template <typename T, int N>
 struct PackOf {
+    typedef T whole __attribute__((ext_vector_type(N)));
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    typedef const type __attribute__((address_space(1))) *source;
+    typedef type __attribute__((address_space(1))) *target;
 };
+
+// Memory of the device, for the compiler: where it loses sight of a pointer's origin it would use accesses that may be LDS as well, and wait for both.
 template <typename T>
-struct PackOf<T, 1> {
-    typedef T type;
-};
-template <typename T, int N>
-using pack_t = typename PackOf<T, N>::type;
+using global_ptr = T __attribute__((address_space(1))) *;
+template <typename T>
+__device__ __forceinline__ global_ptr<T> in_memory(T *p)
+{
+    return (global_ptr<T>)p;
+}
 
 template <typename T, int N>
 __device__ __forceinline__ void load_pack(const T *p, acc_of<T> (&v)[N])
 {
     if constexpr (N == 1) {
-        v[0] = (acc_of<T>)*p;
+        v[0] = (acc_of<T>)*in_memory(p);
     } else {
-        const pack_t<T, N> x = *reinterpret_cast<const pack_t<T, N> *>(p);
+        const typename PackOf<T, N>::whole x = *(typename PackOf<T, N>::source)p;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             v[i] = (acc_of<T>)x[i];
@@ -48,14 +54,22 @@ template <typename T, int N>
 __device__ __forceinline__ void store_pack(T *p, const acc_of<T> (&v)[N])
 {
     if constexpr (N == 1) {
-        *p = (T)v[0];
+        *in_memory(p) = (T)v[0];
     } else {
-        pack_t<T, N> x;
+        typename PackOf<T, N>::whole x;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             x[i] = (T)v[i];
-        *reinterpret_cast<pack_t<T, N> *>(p) = x;
+        *(typename PackOf<T, N>::target)p = x;
     }
+}
+
+// A pointer that the compiler does not see through: in a loop it would keep the address of every element of a partial pack in registers of its own.
+template <typename T>
+__device__ __forceinline__ T *opaque(T *p)
+{
+    asm("" : "+v"(p));
+    return p;
 }
 
 // the first `n` of N elements, the rest zero; `n` may be negative
@@ -65,9 +79,10 @@ __device__ __forceinline__ void load_part(const T *p, int n, acc_of<T> (&v)[N])
     if (n >= N) {
         load_pack<T, N>(p, v);
     } else {
+        p = opaque(p);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = i < n ? (acc_of<T>)p[i] : acc_of<T>(0);
+            v[i] = i < n ? (acc_of<T>)in_memory(p)[i] : acc_of<T>(0);
     }
 }
 template <typename T, int N>
@@ -76,10 +91,11 @@ __device__ __forceinline__ void store_part(T *p, int n, const acc_of<T> (&v)[N])
     if (n >= N) {
         store_pack<T, N>(p, v);
     } else {
+        p = opaque(p);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < n)
-                p[i] = (T)v[i];
+                in_memory(p)[i] = (T)v[i];
     }
 }
 
