@@ -683,6 +683,10 @@ def delta_rule_step(q, k, v, g, beta, state, slots=None, scale=None, out=None):
     """la_delta_rule_step: one token of every sequence: q, k [batch, hk, dk], v [batch, hv, dv], g, beta [batch, hv].  ``state``
     [rows, hv, dk, dv] in float32 is updated in place; sequence n has row ``slots[n]`` (int32, on the GPU), or n.  A slot outside the rows
     gives zeros and updates nothing.  Returns o [batch, hv, dv]."""
+    if _host is not None and out is None:
+        r = _host.delta_rule_step(q, k, v, g, beta, state, slots, scale)
+        if r is not None:
+            return r
     d = _Delta(q, k, v, g, beta, None, lead=1)
     o = torch.empty(v.shape, dtype=v.dtype, device=v.device) if out is None else out
     _shape("out", o, v.shape)
@@ -720,6 +724,10 @@ def _norm_input(x):
 def layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, out=None):
     """la_layer_norm over the last axis of x (whose rows may be a view's, one distance apart).  Returns (y, mean, rstd), the statistics None
     unless ``want_stats``: layer_norm_backward takes them."""
+    if _host is not None and out is None:
+        r = _host.layer_norm(x, weight, bias, eps, want_stats)
+        if r is not None:
+            return r
     dt, rows, n, ld = _norm_input(x)
     wdt = _weights(x, weight, bias)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
@@ -736,6 +744,10 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, out=None):
 def layer_norm_backward(x, y_bar, mean, rstd, weight=None, want_weights=True, out=None, workspace=None):
     """la_layer_norm_backward: (x_bar, weight_bar, bias_bar) from layer_norm's input and statistics; the last two None unless
     ``want_weights``, in weight's dtype (x's where weight is None).  ``out`` may be ``y_bar`` itself."""
+    if _host is not None and out is None and workspace is None:
+        r = _host.layer_norm_backward(x, y_bar, mean, rstd, weight, want_weights)
+        if r is not None:
+            return r
     dt, rows, n, ld = _norm_input(x)
     wdt = _weights(x, weight, None)
     _shape("y_bar", y_bar, x.shape)
@@ -759,6 +771,10 @@ def clip_gradients(grads, max_norm, out=None, workspace=None):
     """la_clip_gradients: scales all tensors of ``grads`` by min(1, max_norm / norm) over all of them, into ``out`` (as many tensors of the same
     shapes and dtypes) or in place.  Returns the norm before it, on the GPU (float64 where a gradient is, else float32); where it is not finite the
     gradients are passed on unchanged."""
+    if _host is not None and workspace is None:
+        r = _host.clip_gradients(grads, max_norm, out)
+        if r is not None:
+            return r
     grads = list(grads)
     outs = grads if out is None else list(out)
     if not grads:

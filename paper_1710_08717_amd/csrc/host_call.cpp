@@ -15,6 +15,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <initializer_list>
 #include <mutex>
 #include <stdexcept>
@@ -40,6 +41,12 @@ struct Lib {
     decltype(&la_potri_backward_ws) potri_backward;
     decltype(&la_sumlogdiag) sumlogdiag;
     decltype(&la_gp_criterion) gp_criterion;
+    decltype(&la_delta_rule_step) delta_rule_step;
+    decltype(&la_layer_norm) layer_norm;
+    decltype(&la_layer_norm_backward_workspace_bytes) layer_norm_backward_workspace_bytes;
+    decltype(&la_layer_norm_backward) layer_norm_backward;
+    decltype(&la_clip_gradients_workspace_bytes) clip_gradients_workspace_bytes;
+    decltype(&la_clip_gradients) clip_gradients;
 } lib;
 bool bound = false;
 
@@ -187,6 +194,20 @@ PyObject *pair(const at::Tensor &a, const at::Tensor &b)
     PyObject *x = wrap(a), *y = x ? wrap(b) : nullptr, *r = y ? PyTuple_Pack(2, x, y) : nullptr;
     Py_XDECREF(x);
     Py_XDECREF(y);
+    return r;
+}
+PyObject *none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+// takes its references over; null where one is
+PyObject *triple(PyObject *x, PyObject *y, PyObject *z)
+{
+    PyObject *r = x && y && z ? PyTuple_Pack(3, x, y, z) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    Py_XDECREF(z);
     return r;
 }
 at::Tensor like(const at::Tensor &t) { return fresh(t.sizes(), t.options()); }
@@ -494,6 +515,215 @@ LA_FUNCTION(gp_criterion, 2)
     return s == LA_OK ? pair(loss, Ab) : nullptr;
 }
 
+// The sequence-layer operators.  Their tensors are float32, bfloat16 or float16 (float64 too for layer norm and clipping) with gates, states and statistics
+// in float32: each has its type asked for.
+bool layer_type(const at::Tensor &t, la_dtype &dt)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: dt = LA_F32; return true;
+    case at::kDouble: dt = LA_F64; return true;
+    case at::kBFloat16: dt = LA_BF16; return true;
+    case at::kHalf: dt = LA_F16; return true;
+    default: return false;
+    }
+}
+
+struct LayerCall : Call {
+    // a plain dense tensor on the call's device (the first one's), or null
+    const at::Tensor *dense(PyObject *o, bool contiguous = true)
+    {
+        if (!THPVariable_CheckExact(o))
+            return nullptr;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.layout() != c10::kStrided || !plain(t) || (contiguous && !t.is_contiguous()) || t.dim() > 8)
+            return nullptr;
+        if (!first) {
+            device = t.get_device();
+            first = &t;
+        } else if (t.get_device() != device) {
+            return nullptr;
+        }
+        return &t;
+    }
+    // None gives true and no tensor
+    bool maybe(PyObject *o, const at::Tensor *&t)
+    {
+        t = o == Py_None ? nullptr : dense(o);
+        return o == Py_None || t;
+    }
+};
+
+// [batch, heads, size] whose heads and elements are dense: elements from one sequence to the next, or -1
+int64_t step_rows(const at::Tensor &t)
+{
+    const int64_t row = t.size(1) * t.size(2);
+    if (t.numel() == 0 || (t.size(2) != 1 && t.stride(2) != 1) || (t.size(1) != 1 && t.stride(1) != t.size(2)))
+        return -1;
+    return t.size(0) == 1 ? row : t.stride(0) >= row ? t.stride(0) : -1;
+}
+
+// (q, k, v, g, beta, state, slots, scale)
+LA_FUNCTION(delta_rule_step, 8)
+{
+    LayerCall c;
+    la_dtype dt;
+    const at::Tensor *q = c.dense(a[0], false), *k = q ? c.dense(a[1], false) : nullptr, *v = k ? c.dense(a[2], false) : nullptr;
+    const at::Tensor *g = v ? c.dense(a[3]) : nullptr, *beta = g ? c.dense(a[4]) : nullptr, *state = beta ? c.dense(a[5]) : nullptr, *slots;
+    double scale;
+    if (!state || !c.maybe(a[6], slots) || !layer_type(*q, dt) || dt == LA_F64 || q->dim() != 3 || v->dim() != 3 || k->sizes() != q->sizes() ||
+        k->scalar_type() != q->scalar_type() || v->scalar_type() != q->scalar_type() || state->dim() != 4)
+        return nullptr;
+    const int64_t batch = q->size(0), hk = q->size(1), dk = q->size(2), hv = v->size(1), dv = v->size(2);
+    if (v->size(0) != batch || hk < 1 || hv < 1 || hv % hk || !small(hv) || !small(dk) || !small(dv))
+        return nullptr;
+    for (const at::Tensor *t : {g, beta})
+        if (t->dim() != 2 || t->size(0) != batch || t->size(1) != hv || t->scalar_type() != at::kFloat)
+            return nullptr;
+    if (state->scalar_type() != at::kFloat || state->size(1) != hv || state->size(2) != dk || state->size(3) != dv ||
+        (slots && (slots->scalar_type() != at::kInt || slots->dim() != 1 || slots->size(0) != batch)))
+        return nullptr;
+    if (a[7] == Py_None)
+        scale = std::pow((double)dk, -0.5);
+    else if (!number(a[7], scale))
+        return nullptr;
+    const int64_t lq = step_rows(*q), lk = step_rows(*k), lv = step_rows(*v);
+    if (lq < 0 || lk < 0 || lv < 0 || !c.here())
+        return nullptr;
+    at::Tensor o;
+    void *st = c.stream();
+    const la_status s = unlocked([&] {
+        o = fresh({batch, hv, dv}, v->options());
+        return lib.delta_rule_step(dt, batch, (int)hk, (int)hv, (int)dk, (int)dv, q->data_ptr(), lq, k->data_ptr(), lk, v->data_ptr(), lv,
+                                   (const float *)g->data_ptr(), (const float *)beta->data_ptr(), scale, (float *)state->data_ptr(), state->size(0),
+                                   slots ? (const int32_t *)slots->data_ptr() : nullptr, o.data_ptr(), st);
+    });
+    return s == LA_OK ? wrap(o) : nullptr;
+}
+
+// the type of weight and bias beside x: x's own, or float32 beside 16 bits
+bool weights_fit(const at::Tensor &x, la_dtype dt, std::initializer_list<const at::Tensor *> w, la_dtype &wdt)
+{
+    wdt = dt;
+    bool seen = false;
+    for (const at::Tensor *t : w)
+        if (t) {
+            la_dtype own;
+            if (t->dim() != 1 || t->size(0) != x.size(-1) || !layer_type(*t, own) || (seen && own != wdt) ||
+                !(own == dt || (own == LA_F32 && (dt == LA_BF16 || dt == LA_F16))))
+                return false;
+            wdt = own;
+            seen = true;
+        }
+    return true;
+}
+
+// (x, weight, bias, eps, want_stats): dense rows
+LA_FUNCTION(layer_norm, 5)
+{
+    LayerCall c;
+    la_dtype dt, wdt;
+    const at::Tensor *x = c.dense(a[0]), *w, *b;
+    double eps;
+    int stats;
+    if (!x || x->dim() < 1 || !c.maybe(a[1], w) || !c.maybe(a[2], b) || !number(a[3], eps) || !flag(a[4], stats) || !layer_type(*x, dt) ||
+        !weights_fit(*x, dt, {w, b}, wdt) || x->size(-1) > INT32_MAX || !c.here())
+        return nullptr;
+    const int64_t rows = leading(*x, 1), n = x->size(-1);
+    at::Tensor y, mean, rstd;
+    void *st = c.stream();
+    const la_status s = unlocked([&] {
+        y = like(*x);
+        if (stats) {
+            const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+            const at::TensorOptions o = x->options().dtype(dt == LA_F64 ? at::kDouble : at::kFloat);
+            mean = fresh(lead, o);
+            rstd = fresh(lead, o);
+        }
+        return lib.layer_norm(dt, wdt, rows, (int)n, n, x->data_ptr(), w ? w->data_ptr() : nullptr, b ? b->data_ptr() : nullptr, eps, y.data_ptr(),
+                              stats ? mean.data_ptr() : nullptr, stats ? rstd.data_ptr() : nullptr, st);
+    });
+    if (s != LA_OK)
+        return nullptr;
+    return stats ? triple(wrap(y), wrap(mean), wrap(rstd)) : triple(wrap(y), none(), none());
+}
+
+// (x, y_bar, mean, rstd, weight, want_weights): dense rows
+LA_FUNCTION(layer_norm_backward, 6)
+{
+    LayerCall c;
+    la_dtype dt, wdt;
+    const at::Tensor *x = c.dense(a[0]), *yb = x ? c.dense(a[1]) : nullptr, *mean = yb ? c.dense(a[2]) : nullptr, *rstd = mean ? c.dense(a[3]) : nullptr, *w;
+    int want;
+    if (!rstd || x->dim() < 1 || !c.maybe(a[4], w) || !flag(a[5], want) || !layer_type(*x, dt) || !weights_fit(*x, dt, {w}, wdt) ||
+        yb->sizes() != x->sizes() || yb->scalar_type() != x->scalar_type() || x->size(-1) > INT32_MAX)
+        return nullptr;
+    const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+    for (const at::Tensor *t : {mean, rstd})
+        if (t->sizes() != lead || t->scalar_type() != (dt == LA_F64 ? at::kDouble : at::kFloat))
+            return nullptr;
+    if (!c.here())
+        return nullptr;
+    const int64_t rows = leading(*x, 1), n = x->size(-1);
+    at::Tensor xb, wb, bb;
+    void *st = c.stream();
+    const la_status s = unlocked([&] {
+        xb = like(*x);
+        if (want) {
+            const at::TensorOptions o = w ? w->options() : x->options();
+            wb = fresh({n}, o);
+            bb = fresh({n}, o);
+        }
+        c.scratch(lib.layer_norm_backward_workspace_bytes(dt, rows, (int)n));
+        return lib.layer_norm_backward(dt, wdt, rows, (int)n, n, x->data_ptr(), yb->data_ptr(), mean->data_ptr(), rstd->data_ptr(),
+                                       w ? w->data_ptr() : nullptr, xb.data_ptr(), want ? wb.data_ptr() : nullptr, want ? bb.data_ptr() : nullptr, c.wp,
+                                       c.wb, st);
+    });
+    if (s != LA_OK)
+        return nullptr;
+    return want ? triple(wrap(xb), wrap(wb), wrap(bb)) : triple(wrap(xb), none(), none());
+}
+
+// (grads, max_norm, out or None): lists of tensors
+LA_FUNCTION(clip_gradients, 3)
+{
+    LayerCall c;
+    double limit;
+    if (!PyList_CheckExact(a[0]) || !number(a[1], limit) || !(a[2] == Py_None || PyList_CheckExact(a[2])))
+        return nullptr;
+    const Py_ssize_t n = PyList_GET_SIZE(a[0]);
+    if (n < 1 || n > INT32_MAX || (a[2] != Py_None && PyList_GET_SIZE(a[2]) != n))
+        return nullptr;
+    std::vector<la_dtype> types(n);
+    std::vector<int64_t> sizes(n);
+    std::vector<const void *> src(n);
+    std::vector<void *> dst(n);
+    std::vector<at::Tensor> held;  // (the lists may change while the GIL is released)
+    held.reserve(2 * n);
+    bool wide = false;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor *x = c.dense(PyList_GET_ITEM(a[0], i)), *y = x && a[2] != Py_None ? c.dense(PyList_GET_ITEM(a[2], i)) : x;
+        if (!x || !y || !layer_type(*x, types[i]) || (y != x && (y->sizes() != x->sizes() || y->scalar_type() != x->scalar_type())))
+            return nullptr;
+        sizes[i] = x->numel();
+        src[i] = x->data_ptr();
+        dst[i] = y->data_ptr();
+        wide |= types[i] == LA_F64;
+        held.push_back(*x);
+        held.push_back(*y);
+    }
+    c.first = &held[0];
+    if (!c.here())
+        return nullptr;
+    at::Tensor norm;
+    void *st = c.stream();
+    const la_status s = unlocked([&] {
+        norm = fresh({}, held[0].options().dtype(wide ? at::kDouble : at::kFloat));
+        c.scratch(lib.clip_gradients_workspace_bytes((int)n, sizes.data()));
+        return lib.clip_gradients((int)n, types.data(), sizes.data(), src.data(), dst.data(), limit, wide ? LA_F64 : LA_F32, norm.data_ptr(), c.wp, c.wb, st);
+    });
+    return s == LA_OK ? wrap(norm) : nullptr;
+}
+
 // bind(path): the library whose functions are called
 PyObject *bind(PyObject *, PyObject *path)
 {
@@ -522,6 +752,12 @@ PyObject *bind(PyObject *, PyObject *path)
     LA_BIND(potri_backward, la_potri_backward_ws);
     LA_BIND(sumlogdiag, la_sumlogdiag);
     LA_BIND(gp_criterion, la_gp_criterion);
+    LA_BIND(delta_rule_step, la_delta_rule_step);
+    LA_BIND(layer_norm, la_layer_norm);
+    LA_BIND(layer_norm_backward_workspace_bytes, la_layer_norm_backward_workspace_bytes);
+    LA_BIND(layer_norm_backward, la_layer_norm_backward);
+    LA_BIND(clip_gradients_workspace_bytes, la_clip_gradients_workspace_bytes);
+    LA_BIND(clip_gradients, la_clip_gradients);
 #undef LA_BIND
     bound = true;
     Py_RETURN_NONE;
@@ -530,7 +766,8 @@ PyObject *bind(PyObject *, PyObject *path)
 #define LA_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LA_METHOD(potrf), LA_METHOD(potrf_backward), LA_METHOD(tri), LA_METHOD(tri_backward), LA_METHOD(syrk), LA_METHOD(syrk_backward),
                          LA_METHOD(gemm2), LA_METHOD(gemm2_backward), LA_METHOD(potri), LA_METHOD(potri_backward), LA_METHOD(sumlogdiag),
-                         LA_METHOD(gp_criterion), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         LA_METHOD(gp_criterion), LA_METHOD(delta_rule_step), LA_METHOD(layer_norm), LA_METHOD(layer_norm_backward),
+                         LA_METHOD(clip_gradients), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_la_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
