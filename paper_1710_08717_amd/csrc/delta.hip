@@ -8,8 +8,9 @@
 //   A_ij = beta_i exp(b_i - b_j) k_i.k_j (j < i),   T = (I + A)^-1,   Z = beta (V - exp(b) K S0),   U = T Z,
 //   P_ij = scale exp(b_i - b_j) q_i.k_j (j <= i),   O = scale exp(b) Q S0 + P U,   S1 = exp(b_last) S0 + K^T exp(b_last - b) U.
 //
-// k_delta_pack forms T, P and the operands' packets for all chunks at once; k_delta_scan walks a sequence's chunks.  Everything after T is separate for
-// every column of V, so a wavefront takes 16 columns and keeps its part of the state in accumulators from the first chunk to the last.
+// k_delta_pack forms T, P T (O = scale exp(b) Q S0 + (P T) Z) and the operands' packets for all chunks at once; k_delta_scan walks a sequence's chunks.
+// Everything after T is separate for every column of V, so two wavefronts take 16 columns and keep the state of them in accumulators from the first chunk
+// to the last.
 #include "delta.hpp"
 
 namespace la {
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
                 for (int r = 0; r < 4; ++r) {
                     const int i = i0 + r;
                     const float e = d.between(i, tj);
-                    m.w.A[i][tj] = tj < i ? d.beta[i] * e * kk[j][r] : 0.0f;
+                    m.w.A[i][tj] = tj < i ? d.walk.beta[i] * e * kk[j][r] : 0.0f;
                     m.w.P[i][tj] = tj <= i ? p.scale * e * qk[j][r] : 0.0f;
                 }
             }
@@ -139,24 +140,21 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
                     m.w.inv[b0 + i][b0 + col] = t[i];
                 }
             }
-        } else {  // the others meanwhile: P and the decays out, zeros right of the diagonal
-            for (int u = wave - 1; u < (SAVE ? 2 : 1) * G::FT; u += 3) {
+        } else {  // the others meanwhile: P^T and the decays out, zeros right of the diagonal
+            if constexpr (SAVE) {
+                for (int u = wave - 1; u < G::FT; u += 3) {
 #pragma unroll
-                for (int i = 0; i < RT; ++i)
+                    for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int s = 0; s < G::CS; ++s) {
-                        if (s <= i / 2 && u == G::lower(i, s)) {
-                            const float *row = &m.w.P[element_of(i, col)][32 * s + 8 * x4];
-                            put_unit<G::NO>(pv, G::P + u, G::FT, join(*reinterpret_cast<const f32x4 *>(row), *reinterpret_cast<const f32x4 *>(row + 4)));
-                        }
-                        if (SAVE && s >= i / 2 && u == G::FT + G::upper(i, s)) {
-                            f32x8 x;
+                        for (int s = 0; s < G::CS; ++s)
+                            if (s >= i / 2 && u == G::upper(i, s)) {
+                                f32x8 x;
 #pragma unroll
-                            for (int r = 0; r < 8; ++r)
-                                x[r] = m.w.P[32 * s + 8 * x4 + r][element_of(i, col)];
-                            put_unit<NX>(pv, G::PTURN + u - G::FT, G::FT, x);
-                        }
-                    }
+                                for (int r = 0; r < 8; ++r)
+                                    x[r] = m.w.P[32 * s + 8 * x4 + r][element_of(i, col)];
+                                put_unit<NX>(pv, G::PTURN + u, G::FT, x);
+                            }
+                }
             }
             if (wave < 3)
                 *reinterpret_cast<f32x4 *>(pv + (wave - 1) * UNIT + 16 * lane) = *reinterpret_cast<const f32x4 *>((const char *)&d + (wave - 1) * UNIT + 16 * lane);
@@ -200,21 +198,40 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
                 m.w.inv[32 + 16 * a1 + 4 * x4 + r][b + col] = -y[r];
         }
         __syncthreads();
-        for (int u = wave; u < (SAVE ? 2 : 1) * G::FT; u += 4) {
+        // P T over A, which is not needed any more: the wavefront's row of 16 x 16 blocks
+        if (wave < C / 16) {
+#pragma unroll
+            for (int j = 0; j < C / 16; ++j) {
+                f32x4 x = {0, 0, 0, 0};
+                if (j <= wave) {
+                    for (int k = j; k <= wave; ++k)
+#pragma unroll
+                        for (int l = 0; l < 4; ++l)
+                            x = __builtin_amdgcn_mfma_f32_16x16x4f32(m.w.P[16 * wave + col][16 * k + 4 * l + x4], m.w.inv[16 * k + 4 * l + x4][16 * j + col], x, 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    m.w.A[16 * wave + 4 * x4 + r][16 * j + col] = x[r];
+            }
+        }
+        __syncthreads();
+        for (int u = wave; u < (SAVE ? 3 : 2) * G::FT; u += 4) {
 #pragma unroll
             for (int i = 0; i < RT; ++i)
 #pragma unroll
                 for (int s = 0; s < G::CS; ++s) {
-                    if (s <= i / 2 && u == G::lower(i, s)) {
-                        const float *row = &m.w.inv[element_of(i, col)][32 * s + 8 * x4];
+                    const float *row = &m.w.inv[element_of(i, col)][32 * s + 8 * x4];
+                    const float *prow = &m.w.A[element_of(i, col)][32 * s + 8 * x4];
+                    if (s <= i / 2 && u == G::lower(i, s))
                         put_unit<NX>(pv, G::TINV + u, G::FT, join(*reinterpret_cast<const f32x4 *>(row), *reinterpret_cast<const f32x4 *>(row + 4)));
-                    }
-                    if (SAVE && s >= i / 2 && u == G::FT + G::upper(i, s)) {
+                    if (s <= i / 2 && u == G::FT + G::lower(i, s))
+                        put_unit<G::NO>(pv, G::P + u - G::FT, G::FT, join(*reinterpret_cast<const f32x4 *>(prow), *reinterpret_cast<const f32x4 *>(prow + 4)));
+                    if (SAVE && s >= i / 2 && u == 2 * G::FT + G::upper(i, s)) {
                         f32x8 x;
 #pragma unroll
                         for (int r = 0; r < 8; ++r)
                             x[r] = m.w.inv[32 * s + 8 * x4 + r][element_of(i, col)];
-                        put_unit<NX>(pv, G::TTURN + u - G::FT, G::FT, x);
+                        put_unit<NX>(pv, G::TTURN + u - 2 * G::FT, G::FT, x);
                     }
                 }
         }
@@ -224,25 +241,31 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 // ---------------------------------------------------------------------------------
 // the walk over a sequence's chunks
 // ---------------------------------------------------------------------------------
-// A chunk has two halves: Z and U from K, Q, T and the decays, then the answers and the new state from P and Kt.  The first half's packets of the next chunk
-// and the second half's of this one come straight to LDS while the first half runs.
-template <typename T, int DKP, int NW, bool SAVE>
-__global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
+// A block takes 64 columns of V: four groups of 16, two wavefronts each.  A wavefront sums K S and Q S over its half of the state's rows, for all tokens, takes
+// the other half's sums for its half of the tokens, forms Z, U and the answers of those, and with everybody's U its half of the new state.  The packets of
+// the next chunk come straight to LDS, into the place of this one's as soon as all have read them.
+template <typename T, int DKP, bool SAVE>
+__global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, KT = G::KT;
-    // first half: K and Q, one unit of decays, T; second half: Kt, P
-    constexpr int LQ = NI * G::FK, LD = 2 * NI * G::FK, LT = LD + 1, FIRST = LT + NX * G::FT, LP = NI * G::FK, SECOND = LP + G::NO * G::FT;
-    constexpr int EACH1 = share<LD, NW>() + share<FIRST - LD, NW>();
-    using In = RowsIn<T, C, NW>;
-    __shared__ __align__(16) char first[2][FIRST * UNIT];
-    __shared__ __align__(16) char second[SECOND * UNIT];
-    __shared__ __align__(16) char vin[C * 16 * NW * sizeof(T)];
-    __shared__ __align__(16) char turn[NW][C * RowsOut<float, C>::ROW];
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NW = 8;
+    constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;  // a wavefront's tiles of tokens and of the state, steps over the state
+    constexpr int LQ = NI * FK, LP = NX * FT;
+    constexpr int EACH_KQ = share<2 * NI * FK, NW>(), EACH_TP = share<(NX + G::NO) * FT, NW>() + 1, EACH_KT = share<NI * FK, NW>();
+    using In = RowsIn<T, C, 4, 512>;
+    constexpr int EX1 = 4 * HT * UNIT > CS * NX * UNIT ? 4 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its U
+    constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's Z; then rows on their way out
+    __shared__ __align__(16) char kq[2 * NI * FK * UNIT];
+    __shared__ __align__(16) char tp[(NX + G::NO) * FT * UNIT];
+    __shared__ __align__(16) char decays[2][UNIT];
+    __shared__ __align__(16) char turned[NI * FK * UNIT];
+    __shared__ __align__(16) char vin[C * 64 * sizeof(T)];
+    __shared__ __align__(16) char ex1_all[4][EX1], ex2_all[4][EX2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
+    const int half = wave >> 2, set = wave & 3;
     const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
     const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int cbase = (slice * NW + wave) * 16, c0 = cbase + col;  // this lane's column of V
+    const int cbase = slice * 64 + set * 16, c0 = cbase + col;  // this lane's column of V
     const bool live = c0 < p.dv, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
@@ -252,41 +275,46 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
     const int chunks = (int)((len + C - 1) / C);
     const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(SAVE) * UNIT), *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(SAVE) * UNIT);
     const int64_t key_step = (int64_t)p.hk * (G::key_units(SAVE) * UNIT), value_step = (int64_t)p.hv * (G::value_units(SAVE) * UNIT);
-    const uint32_t first_at = lds_address(first), second_at = lds_address(second);
-    // (pk, pv: the packets of the chunk that is fetched first)
-    auto fetch_first = [&](const char *k, const char *v, int buffer) {
-        stream_run<LD, NW>(k, first_at + buffer * (FIRST * UNIT), wave);
-        stream_run<FIRST - LD, NW>(v + UNIT, first_at + buffer * (FIRST * UNIT) + LD * UNIT, wave);
+    const uint32_t kq_at = lds_address(kq), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
+    auto fetch_kq = [&](const char *k) { stream_run<2 * NI * FK, NW>(k, kq_at, wave); };
+    auto fetch_tp = [&](const char *v, int buffer) {
+        stream_run<(NX + G::NO) * FT, NW>(v + G::TINV * UNIT, tp_at, wave);
+        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by every wavefront)
     };
-    auto fetch_second = [&](const char *k, const char *v) {
-        stream_run<LP, NW>(k + G::KTURN * UNIT, second_at, wave);
-        stream_run<SECOND - LP, NW>(v + G::P * UNIT, second_at + LP * UNIT, wave);
-    };
-    char *mine = turn[wave];
+    char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In V;
     auto fetch_v = [&](int c) {
-        V.fetch((const T *)p.v + (t0 + (int64_t)c * C) * p.ldv + (int64_t)h * p.dv + slice * NW * 16, p.ldv, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
-                p.dv - slice * NW * 16);
+        V.fetch((const T *)p.v + (t0 + (int64_t)c * C) * p.ldv + (int64_t)h * p.dv + slice * 64, p.ldv, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                p.dv - slice * 64);
     };
+    // rows 16 HT i .. of this wavefront's half of the state
     auto keep_state = [&](int c, const f32x4 *S) {
         if (kept) {
-            float *dst = p.chunk_state + ((slot0 + c) * p.hv + h) * DKP * (int64_t)p.dvp + cbase;
+            float *dst = p.chunk_state + (((slot0 + c) * p.hv + h) * DKP + half * (DKP / 2)) * (int64_t)p.dvp + cbase;
+            constexpr int N = HT > 1 ? HT : 1;
+            if constexpr (N == 1) {
 #pragma unroll
-            for (int i = 0; i < KT / RT; ++i)
-                RowsOut<float, C>::store(mine, dst + (int64_t)i * C * p.dvp, p.dvp, S + i * RT, C, 16);
+                for (int i = 0; i < HK; ++i)
+                    RowsOut<float, 1>::store(mine, dst + (int64_t)(i >> 1) * 32 * p.dvp, p.dvp, S + i, 32, 16, i & 1);
+            } else {
+#pragma unroll
+                for (int i = 0; i < HK / 2; ++i)
+                    RowsOut<float, 2>::store(mine, dst + (int64_t)i * 32 * p.dvp, p.dvp, S + 2 * i, 32, 16);
+            }
         }
     };
 
-    f32x4 S[KT];
+    f32x4 S[HK];
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int t = 0; t < HK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = first_of(t) + r;
-            S[t][r] = p.state0 && live && i < p.dk ? p.state0[state_at + (int64_t)i * p.dv + c0] : 0.0f;
+            const int i = first_of(half * HK + t) + r;
+            S[t][r] = p.state0 && live && i < p.dk ? in_memory(p.state0)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
     if (chunks > 0) {
-        fetch_first(pk, pv, 0);
+        fetch_kq(pk);
+        fetch_tp(pv, 0);
         fetch_v(0);
         if constexpr (SAVE)
             keep_state(0, S);
@@ -294,122 +322,144 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
         wait_loads<0>();
     }
     for (int c = 0; c < chunks; ++c, pk += key_step, pv += value_step) {
-        const char *a = first[c & 1];
         const bool more = c + 1 < chunks;
-        block_barrier();  // the first half's packets and V are there, the chunk before is read
-        f32x4 X[RT], Y[RT], U[RT];
+        block_barrier();  // K, Q and V are there, all have read what the chunk before left
+        stream_run<NI * FK, NW>(pk + G::KTURN * UNIT, turned_at, wave);
+        f32x4 X[RT], Y[RT], U[HT], in[HT], out[HT], beta[HT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                U[i][r] = In::at(vin, first_of(i) + r, 16 * wave + col);
+        for (int i = 0; i < RT; ++i)
             X[i] = Y[i] = f32x4{0, 0, 0, 0};
-        }
         Frag<NI> kf[2][RT], qf[2][RT];
-        Frag<NX> tf[G::FT];
         auto rows_of = [&](int s, Frag<NI> *k, Frag<NI> *q) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                k[i] = unit<NI>(a, G::row(i, s), G::FK);
-                q[i] = unit<NI>(a, LQ + G::row(i, s), G::FK);
+                k[i] = unit<NI>(kq, G::row(i, s), FK);
+                q[i] = unit<NI>(kq, LQ + G::row(i, s), FK);
             }
         };
-        rows_of(0, kf[0], qf[0]);
+        rows_of(half * HS, kf[0], qf[0]);
         issue_point();
-        fetch_second(pk, pv);
-        if (more)
-            fetch_first(pk + key_step, pv + value_step, ~c & 1);
         Frag<NX> f = split<NX>(join(S[0], S[1]));
 #pragma unroll
-        for (int s = 0; s < G::KS; ++s) {
-            if (s + 1 < G::KS) {
-                rows_of(s + 1, kf[~s & 1], qf[~s & 1]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < G::FT; ++i)
-                    tf[i] = unit<NX>(a, LT + i, G::FT);
-            }
+        for (int s = 0; s < HS; ++s) {
+            if (s + 1 < HS)
+                rows_of(half * HS + s + 1, kf[~s & 1], qf[~s & 1]);
             issue_point();
             const Frag<NX> now = f;
-            if (s + 1 < G::KS)
+            if (s + 1 < HS)
                 f = split<NX>(join(S[2 * s + 2], S[2 * s + 3]));
             mma_tiles<3, RT>(X, kf[s & 1], now);
             mma_tiles<G::NO, RT>(Y, qf[s & 1], now);
         }
-        const Decays<C> &d = *reinterpret_cast<const Decays<C> *>(a + (LD - 1) * UNIT);  // (its second unit)
+        // the other half's tokens' sums to the other wavefront; its own sums of this half's
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const f32x4 in = d.four(d.in, first_of(i)), beta = d.four(d.beta, first_of(i));
-            X[i] = beta * (U[i] - in * X[i]);  // Z
-            Y[i] *= p.scale * in;
-            U[i] = f32x4{0, 0, 0, 0};
+        for (int j = 0; j < HT; ++j) {
+            *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 0) * HT + j) * UNIT + 16 * lane) = half ? X[j] : X[HT + j];
+            *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 1) * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
         }
-        mma_tiles<3, (RT < 4 ? RT : 2)>(U, tf, split<NX>(join(X[0], X[1])));
-        if constexpr (RT == 4) {
-            const Frag<NX> f0 = split<NX>(join(X[0], X[1]));
-            const Frag<NX> t2[2] = {tf[2], tf[4]}, t3[2] = {tf[3], tf[5]};
-            mma_tiles<3, 2>(U + 2, t2, f0);
-            mma_tiles<3, 2>(U + 2, t3, split<NX>(join(X[2], X[3])));
+        wait_loads<EACH_KT>();
+        block_barrier();  // (1) sums, T, P T and the decays are there; K and Q are read
+        if (more) {
+            fetch_v(c + 1);
+            fetch_kq(pk + key_step);
         }
+        const Walk<C> &d = *reinterpret_cast<const Walk<C> *>(decays[c & 1]);
+        f32x4 Z[HT], O[HT];
+        Frag<NX> tf[HT][CS];
+        Frag<G::NO> pf[HT][CS];
+#pragma unroll
+        for (int j = 0; j < HT; ++j) {
+            const int i = half * HT + j, first = first_of(i);
+            in[j] = d.four(d.in, first);
+            out[j] = d.four(d.out, first);
+            beta[j] = d.four(d.beta, first);
+            X[j] = (half ? X[HT + j] : X[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((2 * (1 - half) + 0) * HT + j) * UNIT + 16 * lane);
+            Y[j] = (half ? Y[HT + j] : Y[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((2 * (1 - half) + 1) * HT + j) * UNIT + 16 * lane);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                Z[j][r] = In::at(vin, first + r, 16 * set + col);
+        }
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+#pragma unroll
+            for (int s = 0; s < CS; ++s)
+                if (CS == 1 || s == 0 || half) {
+                    const int u = CS == 1 ? half * HT + j : half ? G::lower(2 + j, s) : j;
+                    tf[j][s] = unit<NX>(tp, u, FT);
+                    pf[j][s] = unit<G::NO>(tp, LP + u, FT);
+                }
         const float all = d.all;
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-            S[i] *= all;
-        f32x4 out[RT];
+        for (int j = 0; j < HT; ++j) {
+            Z[j] = beta[j] * (Z[j] - in[j] * X[j]);
+            O[j] = p.scale * in[j] * Y[j];
+            U[j] = f32x4{0, 0, 0, 0};
+        }
+        put_step<RT>(ex2, half, Z);
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            out[i] = d.four(d.out, first_of(i));
+        for (int i = 0; i < HK; ++i)
+            S[i] *= all;
+        block_barrier();  // (2) Z is there, the sums are read
+        auto token_products = [&](int s) {
+            const Frag<NX> z = unit<NX>(ex2, s * NX, 1);
+#pragma unroll
+            for (int j = 0; j < HT; ++j) {
+                mma<3>(U[j], tf[j][s], z);
+                mma<G::NO>(O[j], pf[j][s], z);
+            }
+        };
+        token_products(0);
+        if constexpr (CS > 1)
+            if (half)
+                token_products(1);
+        f32x4 W[HT];
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+            W[j] = out[j] * U[j];
+        put_step<RT>(ex1, half, W);
         if (more)
-            wait_loads<EACH1>();
+            wait_loads<EACH_KQ>();
         else
             wait_loads<0>();
-        block_barrier();  // the second half's packets are there, V is read
+        block_barrier();  // (3) U and Kt are there; T, P T, V and Z are read
         if (more)
-            fetch_v(c + 1);
-        Frag<G::NO> pf[G::FT];
-        Frag<NI> ktf[2][KT];
+            fetch_tp(pv + value_step, ~c & 1);
+        Frag<NI> ktf[CS][HK];
+        Frag<NX> w[CS];
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-            ktf[0][i] = unit<NI>(second, G::turned(i, 0), G::FK);
+        for (int s = 0; s < CS; ++s) {
+            w[s] = unit<NX>(ex1, s * NX, 1);
 #pragma unroll
-        for (int i = 0; i < G::FT; ++i)
-            pf[i] = unit<G::NO>(second, LP + i, G::FT);
+            for (int i = 0; i < HK; ++i)
+                ktf[s][i] = unit<NI>(turned, G::turned(half * HK + i, s), FK);
+        }
         issue_point();
 #pragma unroll
-        for (int s = 0; s < G::CS; ++s) {
-            if (s + 1 < G::CS) {
-#pragma unroll
-                for (int i = 0; i < KT; ++i)
-                    ktf[~s & 1][i] = unit<NI>(second, G::turned(i, s + 1), G::FK);
-                issue_point();
-            }
-            mma_tiles<3, KT>(S, ktf[s & 1], split<NX>(join(U[2 * s] * out[2 * s], U[2 * s + 1] * out[2 * s + 1])));
-            const Frag<NX> u = split<NX>(join(U[2 * s], U[2 * s + 1]));
-#pragma unroll
-            for (int i = 2 * s; i < RT; ++i)
-                mma<G::NO>(Y[i], pf[G::lower(i, s)], u);
-        }
-        wait_loads<0>();  // (before the stores: the next chunk does not wait for them)
-        if (more)
+        for (int s = 0; s < CS; ++s)
+            mma_tiles<3, HK>(S, ktf[s], w[s]);
+        if (more) {
+            wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
             V.put(vin);
-        const int64_t t = t0 + (int64_t)c * C;
-        const int left = (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C);
-        RowsOut<T, C>::store(mine, (T *)p.o + (t * p.hv + h) * p.dv + cbase, (int64_t)p.hv * p.dv, Y, left, p.dv - cbase);
+        }
+        const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);
+        const int64_t left = len - (int64_t)c * C - (HT > 1 ? 32 * half : 0);
+        const int rows = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+        RowsOut<T, HT>::store(mine, (T *)p.o + (t * p.hv + h) * p.dv + cbase, (int64_t)p.hv * p.dv, O, rows, p.dv - cbase, half);
         if constexpr (SAVE) {
             if (kept)
-                RowsOut<float, C>::store(mine, p.chunk_u + ((slot0 + c) * p.hv + h) * C * (int64_t)p.dvp + cbase, p.dvp, U, C, 16);
+                RowsOut<float, HT>::store(mine, p.chunk_u + (((slot0 + c) * p.hv + h) * C + (HT > 1 ? 32 * half : 0)) * (int64_t)p.dvp + cbase, p.dvp, U, 32, 16, half);
             if (more)
                 keep_state(c + 1, S);
         }
     }
     if (p.state1 && live) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int t = 0; t < HK; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = first_of(t) + r;
+                const int i = first_of(half * HK + t) + r;
                 if (i < p.dk)
-                    p.state1[state_at + (int64_t)i * p.dv + c0] = S[t][r];
+                    in_memory(p.state1)[state_at + (int64_t)i * p.dv + c0] = S[t][r];
             }
     }
 }
@@ -417,11 +467,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(DeltaArgs p)
 template <typename T, int DKP, bool SAVE>
 static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
-    constexpr int NW = 4;
     if (p.slots > 0)
         LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
-    p.slices = (p.dv + 16 * NW - 1) / (16 * NW);
-    LA_LAUNCH((k_delta_scan<T, DKP, NW, SAVE>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(64 * NW), 0, st, p);
+    p.slices = (p.dv + 63) / 64;
+    LA_LAUNCH((k_delta_scan<T, DKP, SAVE>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
     return launch_check("delta rule");
 }
 template <typename T, int DKP>

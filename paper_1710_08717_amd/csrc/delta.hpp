@@ -62,7 +62,8 @@ struct DeltaIn<float> {
     static constexpr int NI = 3, C = 32;
 };
 
-constexpr int NX = 3;  // pieces of what is computed
+constexpr int NX = 3;       // pieces of what is computed
+constexpr int UNIT = 1024;  // bytes of an operand of 16 rows, 32 summed elements and one piece, 16 a lane: "a unit"
 
 template <int N>
 struct Frag {
@@ -116,10 +117,32 @@ __device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shuff
 __device__ __forceinline__ int element_of(int i, int m) { return 32 * (i >> 1) + 8 * (m >> 2) + 4 * (i & 1) + (m & 3); }
 __device__ __forceinline__ int first_of(int i) { return 32 * (i >> 1) + 8 * ((threadIdx.x & 63) >> 4) + 4 * (i & 1); }
 
-// Operands of one chunk in the order in which a wavefront reads them: 1024 bytes (16 a lane) for 16 rows, 32 summed elements and one piece, "a unit".
+// Two wavefronts share 16 columns of a walk: wavefront `half` keeps the state's rows and forms the chunk's tokens of its half of the tiles.  What the other one
+// needs of it passes through LDS: operands of a step (32 tokens), whose tiles a wavefront has both (RT = 4, step `half`) or one of (RT = 2).
+template <int RT>
+__device__ __forceinline__ void put_step(char *base, int half, const f32x4 *x)
+{
+    const int lane = threadIdx.x & 63;
+    if constexpr (RT == 4) {
+        const Frag<NX> f = split<NX>(join(x[0], x[1]));
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+            *reinterpret_cast<bf16x8 *>(base + (half * NX + i) * UNIT + 16 * lane) = f.p[i];
+    } else {
+        f32x4 y = x[0];
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            const bf16x4 h = __builtin_convertvector(y, bf16x4);
+            *reinterpret_cast<bf16x4 *>(base + i * UNIT + 16 * lane + 8 * half) = h;
+            if (i + 1 < NX)
+                y -= __builtin_convertvector(h, f32x4);
+        }
+    }
+}
+
+// Operands of one chunk in units, in the order in which a wavefront reads them.
 //   key head:   K (rows tokens, summed over dk), Q, and turned (rows dk, summed over tokens) Kt, for the gradient also Qt
-//   value head: decays (2 units), T and P (lower triangles: steps s <= i / 2 of row tile i), for the gradient also T^T and P^T (s >= i / 2)
-constexpr int UNIT = 1024;
+//   value head: decays (2 units), T and P T (lower triangles: steps s <= i / 2 of row tile i), for the gradient also T^T and P^T (s >= i / 2)
 template <typename T, int DKP>
 struct Pack {
     static constexpr int C = DeltaIn<T>::C, NI = DeltaIn<T>::NI;
@@ -235,17 +258,17 @@ __device__ __forceinline__ f32x8 load8(const T *p, int n)
 
 // The walks' rows of v, o and their like pass through LDS, 16 bytes a lane: a wavefront that is alone on its SIMD pays for every instruction, and an access
 // of 2 bytes is one as well.  Rows past `rows` and columns past `cols` are not touched; nothing has to be aligned.
-// In: 16 NW columns of C rows, by all wavefronts; a chunk ahead into registers, then into LDS.
-template <typename T, int C, int NW>
+// In: 16 NG columns of C rows, by NT lanes; a chunk ahead into registers, then into LDS.
+template <typename T, int C, int NG, int NT>
 struct RowsIn {
-    static constexpr int PE = 16 / sizeof(T), RP = 16 * NW / PE, PER = C * RP / (64 * NW);  // elements of a pack, packs of a row, of a lane
+    static constexpr int PE = 16 / sizeof(T), RP = 16 * NG / PE, PACKS = C * RP, PER = (PACKS + NT - 1) / NT;  // elements of a pack, packs of a row, of a lane
     using Pack16 = PackOf<T, 16 / sizeof(T)>;
     typename Pack16::whole x[PER];
     __device__ __forceinline__ void fetch(const T *src, int64_t ld, int rows, int cols)
     {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int u = k * 64 * NW + threadIdx.x, row = u / RP, c = u % RP * PE;
+            const int u = k * NT + threadIdx.x, row = u < PACKS ? u / RP : rows, c = u % RP * PE;
             const T *at = src + row * ld + c;
             if (row < rows && c + PE <= cols) {
                 x[k] = *(typename Pack16::source)at;
@@ -261,33 +284,36 @@ struct RowsIn {
     {
 #pragma unroll
         for (int k = 0; k < PER; ++k)
-            *reinterpret_cast<typename Pack16::whole *>(lds + (k * 64 * NW + threadIdx.x) * 16) = x[k];
+            if (k * NT + (int)threadIdx.x < PACKS)
+                *reinterpret_cast<typename Pack16::whole *>(lds + (k * NT + threadIdx.x) * 16) = x[k];
     }
-    static __device__ __forceinline__ float at(const char *lds, int row, int col) { return (float)*reinterpret_cast<const T *>(lds + (row * 16 * NW + col) * sizeof(T)); }
+    static __device__ __forceinline__ float at(const char *lds, int row, int col) { return (float)*reinterpret_cast<const T *>(lds + (row * 16 * NG + col) * sizeof(T)); }
 };
-// Out: a wavefront's own 16 columns, C rows of an accumulator.
-template <typename T, int C>
+// Out: a wavefront's 16 columns and N tiles of an accumulator.  Element 4 x + r of tile i is row 8 x + 4 i + r of the 32 that a pair of tiles makes; where N is 1,
+// `odd` says which of the two the tile is.
+template <typename T, int N>
 struct RowsOut {
     static constexpr int ROW = 16 * sizeof(T) + 16, PE = 16 / sizeof(T), RP = sizeof(T);  // bytes of a row with its padding; elements of a pack, packs of a row
+    static constexpr int BYTES = 16 * N * ROW, PER = (16 * N * RP + 63) / 64;                     // packs of a lane
     using Pack16 = PackOf<T, 16 / sizeof(T)>;
     using whole = typename Pack16::whole;
-    static __device__ __forceinline__ void store(char *buf, T *dst, int64_t ld, const f32x4 *x, int rows, int cols)
+    static __device__ __forceinline__ void store(char *buf, T *dst, int64_t ld, const f32x4 *x, int rows, int cols, int odd = 0)
     {
-        const int lane = threadIdx.x & 63, col = lane & 15;
+        const int lane = threadIdx.x & 63, col = lane & 15, x4 = lane >> 4;
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < C / 16; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<T *>(buf + (first_of(i) + r) * ROW + col * sizeof(T)) = (T)x[i][r];
+            for (int r = 0; r < 4; ++r)  // (rows in their order; of a tile alone: 4 x + r)
+                *reinterpret_cast<T *>(buf + ((N == 1 ? 4 * x4 : 32 * (i >> 1) + 8 * x4 + 4 * (i & 1)) + r) * ROW + col * sizeof(T)) = (T)x[i][r];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        whole y[C * RP / 64];
+        whole y[PER];
 #pragma unroll
-        for (int k = 0; k < C * RP / 64; ++k)
-            y[k] = *reinterpret_cast<const whole *>(buf + (k * (64 / RP) + lane / RP) * ROW + lane % RP * 16);
+        for (int k = 0; k < PER; ++k)
+            y[k] = *reinterpret_cast<const whole *>(buf + ((k * (64 / RP) + lane / RP) & (16 * N - 1)) * ROW + lane % RP * 16);
 #pragma unroll
-        for (int k = 0; k < C * RP / 64; ++k) {
-            const int row = k * (64 / RP) + lane / RP, c = lane % RP * PE;
+        for (int k = 0; k < PER; ++k) {
+            const int l = k * (64 / RP) + lane / RP, row = l >= 16 * N ? rows : N == 1 ? 8 * (l >> 2) + 4 * odd + (l & 3) : l, c = lane % RP * PE;
             T *at = dst + row * ld + c;
             if (row < rows && c + PE <= cols) {
                 *(typename Pack16::target)at = y[k];
@@ -301,6 +327,11 @@ struct RowsOut {
         }
     }
 };
+template <int N>
+constexpr int rows_out_bytes()
+{
+    return RowsOut<float, N>::BYTES > RowsOut<bf16_t, N>::BYTES ? RowsOut<float, N>::BYTES : RowsOut<bf16_t, N>::BYTES;
+}
 
 // a sequence's first token and length; what `offsets` holds is kept inside the tokens there are
 __device__ __forceinline__ void sequence(const DeltaArgs &p, int64_t n, int64_t &t0, int64_t &len)
@@ -363,12 +394,17 @@ __device__ __forceinline__ float exp2_of(double x)
 // Decays of a chunk: b_i the sum of g log2(e) up to token i in 64 bits (differences of it are exact enough for any decay; g below -1000 counts as -1000, whose
 // exponential is zero), and what the products take from it.  Tokens past the end have g = beta = 0.  The second unit is what the walks read.
 template <int C>
+struct alignas(16) Walk {
+    float in[C], out[C], beta[C];  // 2^b_i, 2^(b_last - b_i)
+    float all;                     // 2^b_last
+    char rest[UNIT - (3 * C + 1) * 4];
+    static __device__ __forceinline__ f32x4 four(const float *x, int i) { return *reinterpret_cast<const f32x4 *>(x + i); }
+};
+template <int C>
 struct alignas(16) Decays {
     double b[C];
     char rest[UNIT - 8 * C];
-    float in[C], out[C], beta[C];  // 2^b_i, 2^(b_last - b_i)
-    float all;                     // 2^b_last
-    char rest2[UNIT - (3 * C + 1) * 4];
+    Walk<C> walk;
     // by the lanes of one wavefront
     __device__ __forceinline__ void load(const float *g, const float *be, int64_t ld, int len)
     {
@@ -386,15 +422,14 @@ struct alignas(16) Decays {
         const double last = __shfl(x, C - 1, 64);
         if (i < C) {
             b[i] = x;
-            in[i] = exp2_of(x);
-            out[i] = exp2_of(last - x);
-            beta[i] = gate;
+            walk.in[i] = exp2_of(x);
+            walk.out[i] = exp2_of(last - x);
+            walk.beta[i] = gate;
         }
         if (i == 0)
-            all = exp2_of(last);
+            walk.all = exp2_of(last);
     }
     __device__ __forceinline__ float between(int i, int j) const { return __builtin_amdgcn_exp2f((float)(b[i] - b[j])); }
-    static __device__ __forceinline__ f32x4 four(const float *x, int i) { return *reinterpret_cast<const f32x4 *>(x + i); }
 };
 static_assert(sizeof(Decays<64>) == 2 * UNIT && sizeof(Decays<32>) == 2 * UNIT, "two units");
 

@@ -19,24 +19,29 @@
 
 namespace la {
 
-// Two halves a chunk as in the forward walk: K, P^T and the decays, then Q^T, K^T and T^T.
-template <typename T, int DKP, int NW>
-__global__ __launch_bounds__(64 * NW) void k_delta_scan_back(DeltaArgs p)
+// Wavefronts as in the forward walk: the sums of K S1_bar in halves, U_bar and Z_bar of a half of the tokens, a half of the new gradient of the state.
+template <typename T, int DKP>
+__global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, KT = G::KT;
-    constexpr int LD = NI * G::FK, LP = LD + 1, FIRST = LP + NX * G::FT;
-    constexpr int LQ = NI * G::FK, LT = 2 * NI * G::FK, SECOND = LT + NX * G::FT;  // second half: Kt, Qt, T^T
-    constexpr int EACH1 = share<LD, NW>() + 1 + share<FIRST - LP, NW>();
-    using In = RowsIn<T, C, NW>;
-    __shared__ __align__(16) char first[2][FIRST * UNIT];
-    __shared__ __align__(16) char second[SECOND * UNIT];
-    __shared__ __align__(16) char oin[C * 16 * NW * sizeof(T)];
-    __shared__ __align__(16) char turn[NW][C * RowsOut<float, C>::ROW];
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NW = 8;
+    constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;
+    constexpr int LQ = NI * FK, LP = NX * FT;
+    constexpr int EACH_K = share<NI * FK, NW>() + 1, EACH_TP = 2 * share<NX * FT, NW>(), EACH_KT = share<2 * NI * FK, NW>();
+    using In = RowsIn<T, C, 4, 512>;
+    constexpr int EX1 = 2 * HT * UNIT > CS * NX * UNIT ? 2 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its X_bar
+    constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's U_bar; then rows on their way out
+    __shared__ __align__(16) char keys[NI * FK * UNIT];
+    __shared__ __align__(16) char tp[2 * NX * FT * UNIT];  // T^T and P^T
+    __shared__ __align__(16) char decays[2][UNIT];
+    __shared__ __align__(16) char turned[2 * NI * FK * UNIT];  // Kt and Qt
+    __shared__ __align__(16) char oin[C * 64 * sizeof(T)];
+    __shared__ __align__(16) char ex1_all[4][EX1], ex2_all[4][EX2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
+    const int half = wave >> 2, set = wave & 3;
     const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
     const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int cbase = (slice * NW + wave) * 16, c0 = cbase + col;
+    const int cbase = slice * 64 + set * 16, c0 = cbase + col;
     const bool live = c0 < p.dv, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
@@ -47,165 +52,193 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan_back(DeltaArgs p)
     const int64_t key_step = (int64_t)p.hk * (G::key_units(true) * UNIT), value_step = (int64_t)p.hv * (G::value_units(true) * UNIT);
     const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(true) * UNIT) + (chunks - 1) * key_step,
                *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(true) * UNIT) + (chunks - 1) * value_step;
-    const uint32_t first_at = lds_address(first), second_at = lds_address(second);
-    auto fetch_first = [&](const char *k, const char *v, int buffer) {
-        const uint32_t at = first_at + buffer * (FIRST * UNIT);
-        stream_run<LD, NW>(k, at, wave);
-        stream_units<1>(v + UNIT, at + LD * UNIT);  // (the decays: by every wavefront)
-        stream_run<FIRST - LP, NW>(v + G::PTURN * UNIT, at + LP * UNIT, wave);
+    const uint32_t keys_at = lds_address(keys), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
+    auto fetch_k = [&](const char *k, const char *v, int buffer) {
+        stream_run<NI * FK, NW>(k, keys_at, wave);
+        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by every wavefront)
     };
-    auto fetch_second = [&](const char *k, const char *v) {
-        stream_run<LT, NW>(k + G::KTURN * UNIT, second_at, wave);
-        stream_run<SECOND - LT, NW>(v + G::TTURN * UNIT, second_at + LT * UNIT, wave);
+    auto fetch_tp = [&](const char *v) {
+        stream_run<NX * FT, NW>(v + G::TTURN * UNIT, tp_at, wave);
+        stream_run<NX * FT, NW>(v + G::PTURN * UNIT, tp_at + LP * UNIT, wave);
     };
-    char *mine = turn[wave];
+    char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In O;
     auto fetch_o = [&](int c) {
-        O.fetch((const T *)p.o_bar + ((t0 + (int64_t)c * C) * p.hv + h) * p.dv + slice * NW * 16, ldo, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
-                p.dv - slice * NW * 16);
+        O.fetch((const T *)p.o_bar + ((t0 + (int64_t)c * C) * p.hv + h) * p.dv + slice * 64, ldo, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                p.dv - slice * 64);
     };
     auto keep_state = [&](int c, const f32x4 *S) {
         if (kept) {
-            float *dst = p.chunk_state_bar + ((slot0 + c) * p.hv + h) * DKP * (int64_t)p.dvp + cbase;
+            float *dst = p.chunk_state_bar + (((slot0 + c) * p.hv + h) * DKP + half * (DKP / 2)) * (int64_t)p.dvp + cbase;
+            if constexpr (HT == 1) {
 #pragma unroll
-            for (int i = 0; i < KT / RT; ++i)
-                RowsOut<float, C>::store(mine, dst + (int64_t)i * C * p.dvp, p.dvp, S + i * RT, C, 16);
+                for (int i = 0; i < HK; ++i)
+                    RowsOut<float, 1>::store(mine, dst + (int64_t)(i >> 1) * 32 * p.dvp, p.dvp, S + i, 32, 16, i & 1);
+            } else {
+#pragma unroll
+                for (int i = 0; i < HK / 2; ++i)
+                    RowsOut<float, 2>::store(mine, dst + (int64_t)i * 32 * p.dvp, p.dvp, S + 2 * i, 32, 16);
+            }
         }
     };
 
-    f32x4 S[KT];  // the gradient of the state after the chunk
+    f32x4 S[HK];  // the gradient of the state after the chunk
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int t = 0; t < HK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = first_of(t) + r;
-            S[t][r] = p.state1_bar && live && i < p.dk ? p.state1_bar[state_at + (int64_t)i * p.dv + c0] : 0.0f;
+            const int i = first_of(half * HK + t) + r;
+            S[t][r] = p.state1_bar && live && i < p.dk ? in_memory(p.state1_bar)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
     if (chunks > 0) {
-        fetch_first(pk, pv, (chunks - 1) & 1);
+        fetch_k(pk, pv, (chunks - 1) & 1);
+        fetch_tp(pv);
         fetch_o(chunks - 1);
         keep_state(chunks - 1, S);
         O.put(oin);
         wait_loads<0>();
     }
     for (int c = chunks - 1; c >= 0; --c, pk -= key_step, pv -= value_step) {
-        const char *a = first[c & 1];
-        block_barrier();
-        f32x4 Ob[RT], Y[RT], Z[RT];
+        block_barrier();  // K, the decays and O_bar are there, all have read what the chunk before left
+        stream_run<2 * NI * FK, NW>(pk + G::KTURN * UNIT, turned_at, wave);
+        const Walk<C> &d = *reinterpret_cast<const Walk<C> *>(decays[c & 1]);
+        f32x4 Ob[RT], Y[RT];
+        Frag<NI> kf[2][RT];
+        auto rows_of = [&](int s, Frag<NI> *k) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+                k[i] = unit<NI>(keys, G::row(i, s), FK);
+        };
+        rows_of(half * HS, kf[0]);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                Ob[i][r] = In::at(oin, first_of(i) + r, 16 * wave + col);
-            Y[i] = Z[i] = f32x4{0, 0, 0, 0};
+                Ob[i][r] = In::at(oin, first_of(i) + r, 16 * set + col);
+            Y[i] = f32x4{0, 0, 0, 0};
         }
-        Frag<NI> kf[2][RT];
-        Frag<NX> pf[G::FT];
-        auto rows_of = [&](int s, Frag<NI> *k) {
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-                k[i] = unit<NI>(a, G::row(i, s), G::FK);
-        };
-        rows_of(0, kf[0]);
         issue_point();
-        fetch_second(pk, pv);
-        if (c > 0)
-            fetch_first(pk - key_step, pv - value_step, ~c & 1);
         Frag<NX> f = split<NX>(join(S[0], S[1]));
 #pragma unroll
-        for (int s = 0; s < G::KS; ++s) {
-            if (s + 1 < G::KS) {
-                rows_of(s + 1, kf[~s & 1]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < G::FT; ++i)
-                    pf[i] = unit<NX>(a, LP + i, G::FT);
-            }
+        for (int s = 0; s < HS; ++s) {
+            if (s + 1 < HS)
+                rows_of(half * HS + s + 1, kf[~s & 1]);
             issue_point();
             const Frag<NX> now = f;
-            if (s + 1 < G::KS)
+            if (s + 1 < HS)
                 f = split<NX>(join(S[2 * s + 2], S[2 * s + 3]));
             mma_tiles<3, RT>(Y, kf[s & 1], now);
         }
-        const Decays<C> &d = *reinterpret_cast<const Decays<C> *>(a + (LD - 1) * UNIT);  // (its second unit)
-        f32x4 in[RT], beta[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            Y[i] *= d.four(d.out, first_of(i));
-            in[i] = d.four(d.in, first_of(i));
-            beta[i] = d.four(d.beta, first_of(i));
+        for (int j = 0; j < HT; ++j)
+            *reinterpret_cast<f32x4 *>(ex1 + (half * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
+        wait_loads<EACH_KT>();
+        block_barrier();  // (1) sums, T^T and P^T are there; K and O_bar are read
+        if (c > 0) {
+            fetch_o(c - 1);
+            fetch_k(pk - key_step, pv - value_step, ~c & 1);
         }
+        // this half's tokens: row tile i = half HT + j, steps s >= i / 2
+        f32x4 Ub[HT], Z[HT], out[HT], beta[HT], in[HT];
+        Frag<NX> pf[HT][CS], tf[HT][CS];
 #pragma unroll
-        for (int s = 0; s < G::CS; ++s) {
-            const Frag<NI> o = split<NI>(join(Ob[2 * s], Ob[2 * s + 1]));
-#pragma unroll
-            for (int j = 0; j < 2 * s + 2; ++j)
-                mma<3>(Y[j], pf[G::upper(j, s)], o);
+        for (int j = 0; j < HT; ++j) {
+            const int first = first_of(half * HT + j);
+            Ub[j] = (half ? Y[HT + j] : Y[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((1 - half) * HT + j) * UNIT + 16 * lane);
+            out[j] = d.four(d.out, first);
+            in[j] = d.four(d.in, first);
+            beta[j] = d.four(d.beta, first);
+            Z[j] = f32x4{0, 0, 0, 0};
         }
+        auto step_unit = [&](int j, int s) { return CS == 1 ? half * HT + j : half ? G::upper(2 + j, 1) : G::upper(j, s); };
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+#pragma unroll
+            for (int s = 0; s < CS; ++s)
+                if (CS == 1 || s == 1 || !half) {
+                    pf[j][s] = unit<NX>(tp, LP + step_unit(j, s), FT);
+                    tf[j][s] = unit<NX>(tp, step_unit(j, s), FT);
+                }
+#pragma unroll
+        for (int j = 0; j < HT; ++j)
+            Ub[j] *= out[j];
+#pragma unroll
+        for (int s = 0; s < CS; ++s)
+            if (CS == 1 || s == 1 || !half) {
+                const Frag<NI> o = split<NI>(join(Ob[2 * s], Ob[2 * s + 1]));
+#pragma unroll
+                for (int j = 0; j < HT; ++j)
+                    mma<3>(Ub[j], pf[j][s], o);
+            }
+        put_step<RT>(ex2, half, Ub);
         const float all = d.all;
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
+        for (int i = 0; i < HK; ++i)
             S[i] *= all;
+        block_barrier();  // (2) U_bar is there, the sums are read
+#pragma unroll
+        for (int s = 0; s < CS; ++s)
+            if (CS == 1 || s == 1 || !half) {
+                const Frag<NX> u = unit<NX>(ex2, s * NX, 1);
+#pragma unroll
+                for (int j = 0; j < HT; ++j)
+                    mma<3>(Z[j], tf[j][s], u);
+            }
+        // Q^T scale exp(b) O_bar needs nobody else's
+        Frag<NX> w[CS];
+#pragma unroll
+        for (int s = 0; s < CS; ++s)
+            w[s] = split<NX>(join(Ob[2 * s] * (p.scale * d.four(d.in, first_of(2 * s))), Ob[2 * s + 1] * (p.scale * d.four(d.in, first_of(2 * s + 1)))));
+        f32x4 Vb[HT], Xb[HT];
+#pragma unroll
+        for (int j = 0; j < HT; ++j) {
+            Vb[j] = beta[j] * Z[j];
+            Xb[j] = -in[j] * Vb[j];
+        }
+        put_step<RT>(ex1, half, Xb);
         if (c > 0)
-            wait_loads<EACH1>();
+            wait_loads<EACH_K>();
         else
             wait_loads<0>();
-        block_barrier();
+        block_barrier();  // (3) X_bar, Kt and Qt are there; T^T, P^T and U_bar are read
         if (c > 0)
-            fetch_o(c - 1);
-        Frag<NX> tf[G::FT];
-        Frag<NI> ktf[2][KT];
+            fetch_tp(pv - value_step);
         auto turned_of = [&](int from, int s, Frag<NI> *k) {
 #pragma unroll
-            for (int i = 0; i < KT; ++i)
-                k[i] = unit<NI>(second, from + G::turned(i, s), G::FK);
+            for (int i = 0; i < HK; ++i)
+                k[i] = unit<NI>(turned, from + G::turned(half * HK + i, s), FK);
         };
 #pragma unroll
-        for (int i = 0; i < G::FT; ++i)
-            tf[i] = unit<NX>(second, LT + i, G::FT);
-        turned_of(LQ, 0, ktf[0]);
-        issue_point();
-#pragma unroll
-        for (int s = 0; s < G::CS; ++s) {  // Q^T scale exp(b) O_bar, and Z
-            turned_of(s + 1 < G::CS ? LQ : 0, s + 1 < G::CS ? s + 1 : 0, ktf[~s & 1]);
+        for (int s = 0; s < CS; ++s) {
+            Frag<NI> q[HK], k[HK];
+            turned_of(LQ, s, q);
+            const Frag<NX> x = unit<NX>(ex1, s * NX, 1);
+            turned_of(0, s, k);
             issue_point();
-            const Frag<NX> y = split<NX>(join(Y[2 * s], Y[2 * s + 1]));
-#pragma unroll
-            for (int j = 0; j < 2 * s + 2; ++j)
-                mma<3>(Z[j], tf[G::upper(j, s)], y);
-            mma_tiles<3, KT>(S, ktf[s & 1], split<NX>(join(Ob[2 * s] * (p.scale * in[2 * s]), Ob[2 * s + 1] * (p.scale * in[2 * s + 1]))));
+            mma_tiles<3, HK>(S, q, w[s]);
+            mma_tiles<3, HK>(S, k, x);
         }
-        f32x4 Vb[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-            Vb[i] = Z[i] * beta[i];
-#pragma unroll
-        for (int s = 0; s < G::CS; ++s) {
-            if (s + 1 < G::CS) {
-                turned_of(0, s + 1, ktf[(G::CS + s + 1) & 1]);
-                issue_point();
-            }
-            mma_tiles<3, KT>(S, ktf[(G::CS + s) & 1], split<NX>(join(-Vb[2 * s] * in[2 * s], -Vb[2 * s + 1] * in[2 * s + 1])));
-        }
-        wait_loads<0>();  // (before the stores: the next chunk does not wait for them)
-        if (c > 0)
+        if (c > 0) {
+            wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
             O.put(oin);
-        const int64_t t = t0 + (int64_t)c * C;
-        const int left = (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C);
-        RowsOut<T, C>::store(mine, (T *)p.v_bar + (t * p.hv + h) * p.dv + cbase, ldo, Vb, left, p.dv - cbase);
+        }
+        const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);
+        const int64_t left = len - (int64_t)c * C - (HT > 1 ? 32 * half : 0);
+        const int rows = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+        RowsOut<T, HT>::store(mine, (T *)p.v_bar + (t * p.hv + h) * p.dv + cbase, ldo, Vb, rows, p.dv - cbase, half);
         if (kept)
-            RowsOut<float, C>::store(mine, p.chunk_z_bar + ((slot0 + c) * p.hv + h) * C * (int64_t)p.dvp + cbase, p.dvp, Z, C, 16);
+            RowsOut<float, HT>::store(mine, p.chunk_z_bar + (((slot0 + c) * p.hv + h) * C + (HT > 1 ? 32 * half : 0)) * (int64_t)p.dvp + cbase, p.dvp, Z, 32, 16, half);
         if (c > 0)
             keep_state(c - 1, S);
     }
     if (p.state0_bar && live) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int t = 0; t < HK; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = first_of(t) + r;
+                const int i = first_of(half * HK + t) + r;
                 if (i < p.dk)
-                    p.state0_bar[state_at + (int64_t)i * p.dv + c0] = S[t][r];
+                    in_memory(p.state0_bar)[state_at + (int64_t)i * p.dv + c0] = S[t][r];
             }
     }
 }
@@ -423,7 +456,7 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
                     const int x = first_of(i) + r;
                     const float e = before[i][r], f = after[i][r];
                     y.row[i][r] = m ? (e != 0 ? p.scale * e * y.row[i][r] : 0.0f) : (e != 0 && x != mine ? -e * y.row[i][r] : 0.0f);
-                    y.turned[i][r] = m ? (f != 0 ? p.scale * f * y.turned[i][r] : 0.0f) : (f != 0 && x != mine ? -d.beta[x] * f * y.turned[i][r] : 0.0f);
+                    y.turned[i][r] = m ? (f != 0 ? p.scale * f * y.turned[i][r] : 0.0f) : (f != 0 && x != mine ? -d.walk.beta[x] * f * y.turned[i][r] : 0.0f);
                 }
 #pragma unroll
             for (int s = 0; s < CS; ++s) {
@@ -482,10 +515,10 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
         };
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const f32x4 in = d.four(d.in, first_of(i));
+            const f32x4 in = d.walk.four(d.walk.in, first_of(i));
             a1[i] *= p.scale * in;
             a2[i] *= -in;
-            a3[i] *= d.four(d.out, first_of(i));
+            a3[i] *= d.walk.four(d.walk.out, first_of(i));
         }
         dot(3, a3, kt);
 #pragma unroll
@@ -506,7 +539,7 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
         dot(2, a2, kt);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            a3[i] += d.four(d.beta, first_of(i)) * a2[i];
+            a3[i] += d.walk.four(d.walk.beta, first_of(i)) * a2[i];
             Qs[i] += a1[i];
             Ks[i] += a3[i];
         }
@@ -527,8 +560,8 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 #pragma unroll
             for (int w = 0; w < NW; ++w)
                 both += state_box[w];
-            last = wave_sum(last) + d.all * both;
-            double x = lane < C ? whole(0) + 2.0 * d.beta[i] * kh - whole(1) : 0.0;
+            last = wave_sum(last) + d.walk.all * both;
+            double x = lane < C ? whole(0) + 2.0 * d.walk.beta[i] * kh - whole(1) : 0.0;
 #pragma unroll
             for (int s = 1; s < C; s *= 2) {  // from the chunk's end
                 const double y = __shfl_down(x, s, 64);
@@ -558,9 +591,8 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 template <typename T, int DKP>
 static la_status back_t(DeltaArgs &p, hipStream_t st)
 {
-    constexpr int NW = 4;
-    p.slices = (p.dv + 16 * NW - 1) / (16 * NW);
-    LA_LAUNCH((k_delta_scan_back<T, DKP, NW>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(64 * NW), 0, st, p);
+    p.slices = (p.dv + 63) / 64;
+    LA_LAUNCH((k_delta_scan_back<T, DKP>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
     if (p.slots > 0)
         LA_LAUNCH((k_delta_grads<T, DKP>), dim3((unsigned)(p.slots * p.hk)), dim3(4 * DKP), 0, st, p);
     return launch_check("delta rule backward");
