@@ -248,10 +248,10 @@ template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NW = 8;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = 4;  // NL wavefronts load the packets: those of the first half, which have less to do with T
     constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;  // a wavefront's tiles of tokens and of the state, steps over the state
     constexpr int LQ = NI * FK, LP = NX * FT;
-    constexpr int EACH_KQ = share<2 * NI * FK, NW>(), EACH_TP = share<(NX + G::NO) * FT, NW>() + 1, EACH_KT = share<NI * FK, NW>();
+    constexpr int EACH_KQ = share<2 * NI * FK, NL>(), EACH_TP = share<(NX + G::NO) * FT, NL>() + 1, EACH_KT = share<NI * FK, NL>();
     using In = RowsIn<T, C, 4, 512>;
     constexpr int EX1 = 4 * HT * UNIT > CS * NX * UNIT ? 4 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its U
     constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's Z; then rows on their way out
@@ -276,10 +276,10 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(SAVE) * UNIT), *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(SAVE) * UNIT);
     const int64_t key_step = (int64_t)p.hk * (G::key_units(SAVE) * UNIT), value_step = (int64_t)p.hv * (G::value_units(SAVE) * UNIT);
     const uint32_t kq_at = lds_address(kq), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
-    auto fetch_kq = [&](const char *k) { stream_run<2 * NI * FK, NW>(k, kq_at, wave); };
+    auto fetch_kq = [&](const char *k) { stream_run<2 * NI * FK, NL>(k, kq_at, wave); };
     auto fetch_tp = [&](const char *v, int buffer) {
-        stream_run<(NX + G::NO) * FT, NW>(v + G::TINV * UNIT, tp_at, wave);
-        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by every wavefront)
+        stream_run<(NX + G::NO) * FT, NL>(v + G::TINV * UNIT, tp_at, wave);
+        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by each of them)
     };
     char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In V;
@@ -304,6 +304,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
         }
     };
 
+    if (half)  // what the others wait for
+        __builtin_amdgcn_s_setprio(1);
     f32x4 S[HK];
 #pragma unroll
     for (int t = 0; t < HK; ++t)
@@ -313,8 +315,10 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
             S[t][r] = p.state0 && live && i < p.dk ? in_memory(p.state0)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
     if (chunks > 0) {
-        fetch_kq(pk);
-        fetch_tp(pv, 0);
+        if (!half) {
+            fetch_kq(pk);
+            fetch_tp(pv, 0);
+        }
         fetch_v(0);
         if constexpr (SAVE)
             keep_state(0, S);
@@ -324,7 +328,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     for (int c = 0; c < chunks; ++c, pk += key_step, pv += value_step) {
         const bool more = c + 1 < chunks;
         block_barrier();  // K, Q and V are there, all have read what the chunk before left
-        stream_run<NI * FK, NW>(pk + G::KTURN * UNIT, turned_at, wave);
+        if (!half)
+            stream_run<NI * FK, NL>(pk + G::KTURN * UNIT, turned_at, wave);
         f32x4 X[RT], Y[RT], U[HT], in[HT], out[HT], beta[HT];
 #pragma unroll
         for (int i = 0; i < RT; ++i)
@@ -357,11 +362,13 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
             *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 0) * HT + j) * UNIT + 16 * lane) = half ? X[j] : X[HT + j];
             *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 1) * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
         }
-        wait_loads<EACH_KT>();
+        if (!half)
+            wait_loads<EACH_KT>();
         block_barrier();  // (1) sums, T, P T and the decays are there; K and Q are read
         if (more) {
             fetch_v(c + 1);
-            fetch_kq(pk + key_step);
+            if (!half)
+                fetch_kq(pk + key_step);
         }
         const Walk<C> &d = *reinterpret_cast<const Walk<C> *>(decays[c & 1]);
         f32x4 Z[HT], O[HT];
@@ -417,12 +424,14 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
         for (int j = 0; j < HT; ++j)
             W[j] = out[j] * U[j];
         put_step<RT>(ex1, half, W);
-        if (more)
-            wait_loads<EACH_KQ>();
-        else
-            wait_loads<0>();
+        if (!half) {
+            if (more)
+                wait_loads<EACH_KQ>();
+            else
+                wait_loads<0>();
+        }
         block_barrier();  // (3) U and Kt are there; T, P T, V and Z are read
-        if (more)
+        if (more && !half)
             fetch_tp(pv + value_step, ~c & 1);
         Frag<NI> ktf[CS][HK];
         Frag<NX> w[CS];
@@ -438,7 +447,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
         for (int s = 0; s < CS; ++s)
             mma_tiles<3, HK>(S, ktf[s], w[s]);
         if (more) {
-            wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
+            if (!half)
+                wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
             V.put(vin);
         }
         const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);

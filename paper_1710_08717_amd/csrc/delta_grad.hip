@@ -24,10 +24,10 @@ template <typename T, int DKP>
 __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NW = 8;
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = 4;  // NL wavefronts load the packets: those of the second half, which have less to do with T^T
     constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;
     constexpr int LQ = NI * FK, LP = NX * FT;
-    constexpr int EACH_K = share<NI * FK, NW>() + 1, EACH_TP = 2 * share<NX * FT, NW>(), EACH_KT = share<2 * NI * FK, NW>();
+    constexpr int EACH_K = share<NI * FK, NL>() + 1, EACH_TP = 2 * share<NX * FT, NL>(), EACH_KT = share<2 * NI * FK, NL>();
     using In = RowsIn<T, C, 4, 512>;
     constexpr int EX1 = 2 * HT * UNIT > CS * NX * UNIT ? 2 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its X_bar
     constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's U_bar; then rows on their way out
@@ -54,12 +54,12 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
                *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(true) * UNIT) + (chunks - 1) * value_step;
     const uint32_t keys_at = lds_address(keys), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
     auto fetch_k = [&](const char *k, const char *v, int buffer) {
-        stream_run<NI * FK, NW>(k, keys_at, wave);
-        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by every wavefront)
+        stream_run<NI * FK, NL>(k, keys_at, set);
+        stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by each of them)
     };
     auto fetch_tp = [&](const char *v) {
-        stream_run<NX * FT, NW>(v + G::TTURN * UNIT, tp_at, wave);
-        stream_run<NX * FT, NW>(v + G::PTURN * UNIT, tp_at + LP * UNIT, wave);
+        stream_run<NX * FT, NL>(v + G::TTURN * UNIT, tp_at, set);
+        stream_run<NX * FT, NL>(v + G::PTURN * UNIT, tp_at + LP * UNIT, set);
     };
     char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In O;
@@ -82,6 +82,8 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
         }
     };
 
+    if (!half)  // what the others wait for
+        __builtin_amdgcn_s_setprio(1);
     f32x4 S[HK];  // the gradient of the state after the chunk
 #pragma unroll
     for (int t = 0; t < HK; ++t)
@@ -91,8 +93,10 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
             S[t][r] = p.state1_bar && live && i < p.dk ? in_memory(p.state1_bar)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
         }
     if (chunks > 0) {
-        fetch_k(pk, pv, (chunks - 1) & 1);
-        fetch_tp(pv);
+        if (half) {
+            fetch_k(pk, pv, (chunks - 1) & 1);
+            fetch_tp(pv);
+        }
         fetch_o(chunks - 1);
         keep_state(chunks - 1, S);
         O.put(oin);
@@ -100,7 +104,8 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
     }
     for (int c = chunks - 1; c >= 0; --c, pk -= key_step, pv -= value_step) {
         block_barrier();  // K, the decays and O_bar are there, all have read what the chunk before left
-        stream_run<2 * NI * FK, NW>(pk + G::KTURN * UNIT, turned_at, wave);
+        if (half)
+            stream_run<2 * NI * FK, NL>(pk + G::KTURN * UNIT, turned_at, set);
         const Walk<C> &d = *reinterpret_cast<const Walk<C> *>(decays[c & 1]);
         f32x4 Ob[RT], Y[RT];
         Frag<NI> kf[2][RT];
@@ -132,11 +137,13 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
 #pragma unroll
         for (int j = 0; j < HT; ++j)
             *reinterpret_cast<f32x4 *>(ex1 + (half * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
-        wait_loads<EACH_KT>();
+        if (half)
+            wait_loads<EACH_KT>();
         block_barrier();  // (1) sums, T^T and P^T are there; K and O_bar are read
         if (c > 0) {
             fetch_o(c - 1);
-            fetch_k(pk - key_step, pv - value_step, ~c & 1);
+            if (half)
+                fetch_k(pk - key_step, pv - value_step, ~c & 1);
         }
         // this half's tokens: row tile i = half HT + j, steps s >= i / 2
         f32x4 Ub[HT], Z[HT], out[HT], beta[HT], in[HT];
@@ -196,12 +203,14 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
             Xb[j] = -in[j] * Vb[j];
         }
         put_step<RT>(ex1, half, Xb);
-        if (c > 0)
-            wait_loads<EACH_K>();
-        else
-            wait_loads<0>();
+        if (half) {
+            if (c > 0)
+                wait_loads<EACH_K>();
+            else
+                wait_loads<0>();
+        }
         block_barrier();  // (3) X_bar, Kt and Qt are there; T^T, P^T and U_bar are read
-        if (c > 0)
+        if (c > 0 && half)
             fetch_tp(pv - value_step);
         auto turned_of = [&](int from, int s, Frag<NI> *k) {
 #pragma unroll
@@ -219,7 +228,8 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
             mma_tiles<3, HK>(S, k, x);
         }
         if (c > 0) {
-            wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
+            if (half)
+                wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
             O.put(oin);
         }
         const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);
