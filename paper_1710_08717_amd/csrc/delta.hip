@@ -244,19 +244,24 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 // A block takes 64 columns of V: four groups of 16, two wavefronts each.  A wavefront sums K S and Q S over its half of the state's rows, for all tokens, takes
 // the other half's sums for its half of the tokens, forms Z, U and the answers of those, and with everybody's U its half of the new state.  The packets of
 // the next chunk come straight to LDS, into the place of this one's as soon as all have read them.
-template <typename T, int DKP, bool SAVE>
+//
+// Where sequences and heads are too few to fill the chip, a sequence is walked in segments side by side.  The state after a segment is M S + N with S the state
+// before it: MAP blocks find N (the walk from a state of zeros) and the columns of M (from the unit vectors, with V zero), without answers;
+// k_delta_join goes from segment to segment; then every segment is walked from its own state.
+template <typename T, int DKP, bool SAVE, bool MAP>
 __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
     constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = 4;  // NL wavefronts load the packets: those of the first half, which have less to do with T
     constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;  // a wavefront's tiles of tokens and of the state, steps over the state
     constexpr int LQ = NI * FK, LP = NX * FT;
-    constexpr int EACH_KQ = share<2 * NI * FK, NL>(), EACH_TP = share<(NX + G::NO) * FT, NL>() + 1, EACH_KT = share<NI * FK, NL>();
+    constexpr int NKQ = (MAP ? 1 : 2) * NI * FK, NTP = (MAP ? NX : NX + G::NO) * FT;
+    constexpr int EACH_KQ = share<NKQ, NL>(), EACH_TP = share<NTP, NL>() + 1, EACH_KT = share<NI * FK, NL>();
     using In = RowsIn<T, C, 4, 512>;
     constexpr int EX1 = 4 * HT * UNIT > CS * NX * UNIT ? 4 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its U
     constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's Z; then rows on their way out
-    __shared__ __align__(16) char kq[2 * NI * FK * UNIT];
-    __shared__ __align__(16) char tp[(NX + G::NO) * FT * UNIT];
+    __shared__ __align__(16) char kq[NKQ * UNIT];
+    __shared__ __align__(16) char tp[NTP * UNIT];
     __shared__ __align__(16) char decays[2][UNIT];
     __shared__ __align__(16) char turned[NI * FK * UNIT];
     __shared__ __align__(16) char vin[C * 64 * sizeof(T)];
@@ -264,28 +269,46 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
     const int half = wave >> 2, set = wave & 3;
     const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
-    const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int cbase = slice * 64 + set * 16, c0 = cbase + col;  // this lane's column of V
-    const bool live = c0 < p.dv, kept = cbase < p.dvp;
+    const int64_t sg = blockIdx.x / p.slices / p.hv, n = p.seg ? segment_sequence<C>(p, sg) : sg;
+    const int vslices = (p.dv + 63) / 64;
+    const bool unit_columns = MAP && slice >= vslices;
+    const int sbase = (unit_columns ? slice - vslices : slice) * 64, cbase = sbase + set * 16, c0 = cbase + col;  // this lane's column of V (or of M)
+    const int width = unit_columns ? p.dk : p.dv;
+    const bool live = c0 < width, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
     const int hk = h / (p.hv / p.hk);
     const int64_t state_at = (n * p.hv + h) * p.dk * (int64_t)p.dv;
-    const int64_t slot0 = first_slot<C>(p, n, t0);
-    const int chunks = (int)((len + C - 1) / C);
+    int64_t slot0 = first_slot<C>(p, n, t0);
+    int chunks = (int)((len + C - 1) / C), part = 0;
+    bool last = true;
+    if (p.seg) {  // chunks seg part .. of the sequence
+        part = (int)(sg - first_segment<C>(p, n, t0));
+        const int from = part * p.seg;
+        if (part < 0 || (part > 0 && from >= chunks))
+            return;
+        last = from + p.seg >= chunks;
+        if (MAP && (last || (part == 0 && unit_columns)))  // (nobody asks for those)
+            return;
+        chunks = last ? chunks - from : p.seg;
+        slot0 += from;
+        t0 += (int64_t)from * C;
+        len -= (int64_t)from * C;
+        len = last ? len : (int64_t)chunks * C;
+    }
     const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(SAVE) * UNIT), *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(SAVE) * UNIT);
     const int64_t key_step = (int64_t)p.hk * (G::key_units(SAVE) * UNIT), value_step = (int64_t)p.hv * (G::value_units(SAVE) * UNIT);
     const uint32_t kq_at = lds_address(kq), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
-    auto fetch_kq = [&](const char *k) { stream_run<2 * NI * FK, NL>(k, kq_at, wave); };
+    auto fetch_kq = [&](const char *k) { stream_run<NKQ, NL>(k, kq_at, wave); };
     auto fetch_tp = [&](const char *v, int buffer) {
-        stream_run<(NX + G::NO) * FT, NL>(v + G::TINV * UNIT, tp_at, wave);
+        stream_run<NTP, NL>(v + G::TINV * UNIT, tp_at, wave);
         stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by each of them)
     };
     char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In V;
     auto fetch_v = [&](int c) {
-        V.fetch((const T *)p.v + (t0 + (int64_t)c * C) * p.ldv + (int64_t)h * p.dv + slice * 64, p.ldv, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
-                p.dv - slice * 64);
+        V.fetch((const T *)p.v + (t0 + (int64_t)c * C) * p.ldv + (int64_t)h * p.dv + sbase, p.ldv, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                unit_columns ? 0 : p.dv - sbase);
     };
     // rows 16 HT i .. of this wavefront's half of the state
     auto keep_state = [&](int c, const f32x4 *S) {
@@ -312,7 +335,12 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = first_of(half * HK + t) + r;
-            S[t][r] = p.state0 && live && i < p.dk ? in_memory(p.state0)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
+            if (part == 0)
+                S[t][r] = p.state0 && live && i < p.dk ? in_memory(p.state0)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
+            else if (MAP)
+                S[t][r] = unit_columns && i == c0 ? 1.0f : 0.0f;
+            else
+                S[t][r] = kept ? in_memory(p.seg_state)[((sg * p.hv + h) * DKP + i) * p.dvp + c0] : 0.0f;
         }
     if (chunks > 0) {
         if (!half) {
@@ -320,7 +348,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
             fetch_tp(pv, 0);
         }
         fetch_v(0);
-        if constexpr (SAVE)
+        if constexpr (SAVE && !MAP)
             keep_state(0, S);
         V.put(vin);
         wait_loads<0>();
@@ -339,7 +367,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 k[i] = unit<NI>(kq, G::row(i, s), FK);
-                q[i] = unit<NI>(kq, LQ + G::row(i, s), FK);
+                if constexpr (!MAP)
+                    q[i] = unit<NI>(kq, LQ + G::row(i, s), FK);
             }
         };
         rows_of(half * HS, kf[0], qf[0]);
@@ -354,13 +383,15 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
             if (s + 1 < HS)
                 f = split<NX>(join(S[2 * s + 2], S[2 * s + 3]));
             mma_tiles<3, RT>(X, kf[s & 1], now);
-            mma_tiles<G::NO, RT>(Y, qf[s & 1], now);
+            if constexpr (!MAP)
+                mma_tiles<G::NO, RT>(Y, qf[s & 1], now);
         }
         // the other half's tokens' sums to the other wavefront; its own sums of this half's
 #pragma unroll
         for (int j = 0; j < HT; ++j) {
             *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 0) * HT + j) * UNIT + 16 * lane) = half ? X[j] : X[HT + j];
-            *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 1) * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
+            if constexpr (!MAP)
+                *reinterpret_cast<f32x4 *>(ex1 + ((2 * half + 1) * HT + j) * UNIT + 16 * lane) = half ? Y[j] : Y[HT + j];
         }
         if (!half)
             wait_loads<EACH_KT>();
@@ -381,7 +412,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
             out[j] = d.four(d.out, first);
             beta[j] = d.four(d.beta, first);
             X[j] = (half ? X[HT + j] : X[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((2 * (1 - half) + 0) * HT + j) * UNIT + 16 * lane);
-            Y[j] = (half ? Y[HT + j] : Y[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((2 * (1 - half) + 1) * HT + j) * UNIT + 16 * lane);
+            if constexpr (!MAP)
+                Y[j] = (half ? Y[HT + j] : Y[j]) + *reinterpret_cast<const f32x4 *>(ex1 + ((2 * (1 - half) + 1) * HT + j) * UNIT + 16 * lane);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 Z[j][r] = In::at(vin, first + r, 16 * set + col);
@@ -393,7 +425,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
                 if (CS == 1 || s == 0 || half) {
                     const int u = CS == 1 ? half * HT + j : half ? G::lower(2 + j, s) : j;
                     tf[j][s] = unit<NX>(tp, u, FT);
-                    pf[j][s] = unit<G::NO>(tp, LP + u, FT);
+                    if constexpr (!MAP)
+                        pf[j][s] = unit<G::NO>(tp, LP + u, FT);
                 }
         const float all = d.all;
 #pragma unroll
@@ -412,7 +445,8 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
 #pragma unroll
             for (int j = 0; j < HT; ++j) {
                 mma<3>(U[j], tf[j][s], z);
-                mma<G::NO>(O[j], pf[j][s], z);
+                if constexpr (!MAP)
+                    mma<G::NO>(O[j], pf[j][s], z);
             }
         };
         token_products(0);
@@ -451,18 +485,32 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
                 wait_loads<EACH_TP>();  // (before the stores: the next chunk does not wait for them)
             V.put(vin);
         }
-        const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);
-        const int64_t left = len - (int64_t)c * C - (HT > 1 ? 32 * half : 0);
-        const int rows = (int)(left < 0 ? 0 : left < 32 ? left : 32);
-        RowsOut<T, HT>::store(mine, (T *)p.o + (t * p.hv + h) * p.dv + cbase, (int64_t)p.hv * p.dv, O, rows, p.dv - cbase, half);
-        if constexpr (SAVE) {
+        if constexpr (!MAP) {
+            const int64_t t = t0 + (int64_t)c * C + (HT > 1 ? 32 * half : 0);
+            const int64_t left = len - (int64_t)c * C - (HT > 1 ? 32 * half : 0);
+            const int rows = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+            RowsOut<T, HT>::store(mine, (T *)p.o + (t * p.hv + h) * p.dv + cbase, (int64_t)p.hv * p.dv, O, rows, p.dv - cbase, half);
+        }
+        if constexpr (SAVE && !MAP) {
             if (kept)
                 RowsOut<float, HT>::store(mine, p.chunk_u + (((slot0 + c) * p.hv + h) * C + (HT > 1 ? 32 * half : 0)) * (int64_t)p.dvp + cbase, p.dvp, U, 32, 16, half);
             if (more)
                 keep_state(c + 1, S);
         }
     }
-    if (p.state1 && live) {
+    if constexpr (MAP) {  // N to where the next segment's state will be, or M
+        float *to = unit_columns ? p.seg_map + (sg * p.hv + h) * DKP * (int64_t)DKP : p.seg_state + ((sg + 1) * p.hv + h) * DKP * (int64_t)p.dvp;
+        const int ld = unit_columns ? DKP : p.dvp;
+        if (cbase < ld) {
+#pragma unroll
+            for (int t = 0; t < HK; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    in_memory(to)[(int64_t)(first_of(half * HK + t) + r) * ld + c0] = S[t][r];
+        }
+        return;
+    }
+    if (p.state1 && live && last) {
 #pragma unroll
         for (int t = 0; t < HK; ++t)
 #pragma unroll
@@ -474,13 +522,67 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     }
 }
 
+// From the state before a segment to the one after it, M S + N, over a sequence's segments: 16 columns of one head a wavefront.
+template <int C, int DKP>
+__global__ __launch_bounds__(64) void k_delta_join(DeltaArgs p)
+{
+    constexpr int KT = DKP / 16, KS = DKP / 32;
+    const int lane = threadIdx.x, col = lane & 15, x4 = lane >> 4, slices = p.dvp / 16;
+    const int c0 = (int)(blockIdx.x % slices) * 16 + col, h = blockIdx.x / slices % p.hv;
+    const int64_t n = blockIdx.x / slices / p.hv;
+    int64_t t0, len;
+    sequence(p, n, t0, len);
+    const int64_t sg = first_segment<C>(p, n, t0);
+    const int parts = (int)((len + (int64_t)C * p.seg - 1) / ((int64_t)C * p.seg));
+    if (parts < 3)
+        return;  // (the state before segment 1 is there)
+    f32x4 S[KT];
+    auto at = [&](int64_t g) { return in_memory(p.seg_state + ((g * p.hv + h) * DKP) * (int64_t)p.dvp + c0); };
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            S[i][r] = at(sg + 1)[(int64_t)(first_of(i) + r) * p.dvp];
+    for (int g = 1; g + 1 < parts; ++g) {
+        const float *M = p.seg_map + ((sg + g) * p.hv + h) * DKP * (int64_t)DKP;
+        Frag<NX> f[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            f[s] = split<NX>(join(S[2 * s], S[2 * s + 1]));
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+            f32x8 m[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                m[s] = load8<float>(M + element_of(i, col) * DKP + 32 * s + 8 * x4, 8);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[i][r] = at(sg + g + 1)[(int64_t)(first_of(i) + r) * p.dvp];
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                mma<3>(S[i], split<NX>(m[s]), f[s]);
+        }
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                at(sg + g + 1)[(int64_t)(first_of(i) + r) * p.dvp] = S[i][r];
+    }
+}
+
 template <typename T, int DKP, bool SAVE>
 static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
     if (p.slots > 0)
         LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
-    p.slices = (p.dv + 63) / 64;
-    LA_LAUNCH((k_delta_scan<T, DKP, SAVE>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
+    const int vslices = (p.dv + 63) / 64;
+    if (p.seg) {
+        p.slices = vslices + (p.dk + 63) / 64;
+        LA_LAUNCH((k_delta_scan<T, DKP, SAVE, true>), dim3((unsigned)(p.segs * p.hv * p.slices)), dim3(512), 0, st, p);
+        LA_LAUNCH((k_delta_join<Pack<T, DKP>::C, DKP>), dim3((unsigned)(p.batch * p.hv * (p.dvp / 16))), dim3(64), 0, st, p);
+    }
+    p.slices = vslices;
+    LA_LAUNCH((k_delta_scan<T, DKP, SAVE, false>), dim3((unsigned)((p.seg ? p.segs : p.batch) * p.hv * p.slices)), dim3(512), 0, st, p);
     return launch_check("delta rule");
 }
 template <typename T, int DKP>
@@ -610,6 +712,7 @@ static la_status step_t(DeltaStepArgs &p, int64_t batch, hipStream_t st)
 // sizes and buffers
 // ---------------------------------------------------------------------------------
 constexpr int DELTA_MAX_DK = 128, DELTA_MAX_DV = 1024;
+constexpr int64_t COMPUTE_UNITS = 256;
 constexpr int64_t DELTA_MAX_ROW = 1 << 24;  // elements of one token's row of v
 
 struct DeltaSizes {
@@ -617,7 +720,10 @@ struct DeltaSizes {
     int c = 0, dkp = 0, dvp = 0;
     size_t key[2] = {}, value[2] = {};  // bytes of the packets, without and with what the gradient takes
     size_t state = 0, u = 0;            // of the states and of U by slot and value head
-    size_t packets(bool save) const { return key[save] + value[save]; }
+    int seg = 0;                        // chunks of a segment, 0 where sequences are walked whole
+    int64_t segs = 0;
+    size_t seg_state = 0, seg_map = 0;
+    size_t packets(bool save) const { return key[save] + value[save] + seg_state + seg_map; }
     size_t saved() const { return packets(true) + state + u; }
     size_t grad() const { return state + u; }  // the state's gradient, Z's gradient
 };
@@ -658,6 +764,19 @@ static la_status delta_sizes(la_dtype dt, int64_t batch, int64_t tokens, int hk,
     if (z.slots > most / hv || batch > most / hv / ((dv + 15) / 16))  // blocks of one launch
         return LA_ERR_UNSUPPORTED;
     const size_t heads = (size_t)z.slots * hv;
+    // Segments where whole sequences would leave more than two thirds of the compute units idle, as many as fill them, of 8 chunks at least and up to 8 of a
+    // sequence of the average length: a sequence of g segments takes the time of about 2 / g of it (16 heads of 128, 8192 tokens, bf16: %SEG%).
+    const int64_t blocks = batch * hv * ((dv + 63) / 64);
+    if (blocks > 0 && blocks * 3 <= COMPUTE_UNITS) {
+        const int64_t each = (z.all / batch + z.c - 1) / z.c, most_parts = COMPUTE_UNITS / blocks < 8 ? COMPUTE_UNITS / blocks : 8;
+        const int64_t seg = (each + most_parts - 1) / most_parts;
+        if (each >= 24) {
+            z.seg = (int)(seg < 8 ? 8 : seg);
+            z.segs = packed ? z.slots / z.seg + batch : batch * ((each + z.seg - 1) / z.seg);
+            z.seg_state = align_up((size_t)(z.segs + 1) * hv * z.dkp * z.dvp * 4);
+            z.seg_map = align_up((size_t)z.segs * hv * z.dkp * z.dkp * 4);
+        }
+    }
     z.state = align_up(heads * z.dkp * z.dvp * 4);
     z.u = align_up(heads * z.c * z.dvp * 4);
     return LA_OK;
@@ -667,8 +786,12 @@ static void place_packets(DeltaArgs &p, const DeltaSizes &z, void *base, bool sa
 {
     p.pack_k = (char *)base;
     p.pack_v = p.pack_k + z.key[save];
+    p.seg = z.seg;
+    p.segs = z.segs;
+    p.seg_state = (float *)(p.pack_v + z.value[save]);
+    p.seg_map = (float *)((char *)p.seg_state + z.seg_state);
     if (save) {
-        p.chunk_state = (float *)(p.pack_v + z.value[save]);
+        p.chunk_state = (float *)((char *)p.seg_map + z.seg_map);
         p.chunk_u = (float *)((char *)p.chunk_state + z.state);
     }
 }

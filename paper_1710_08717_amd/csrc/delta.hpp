@@ -45,6 +45,11 @@ struct DeltaArgs {
     void *q_bar, *k_bar, *v_bar;
     float *g_bar, *beta_bar, *state0_bar;
     int slices;  // blocks over dv
+    // Few sequences and heads: they are walked in segments of `seg` chunks (0: whole).  By segment slot and value head: the state before it [DKP][dvp], and
+    // the matrix [DKP][DKP] by which a segment's last state depends on its first.
+    int seg;
+    int64_t segs;
+    float *seg_state, *seg_map;
 };
 
 template <typename T>
@@ -382,6 +387,29 @@ __device__ __forceinline__ bool slot_chunk(const DeltaArgs &p, int64_t slot, int
     const int64_t left = all - c * C;
     len = (int)(left < C ? left : C);
     return true;
+}
+
+// The slot of a sequence's first segment, by first_slot's trick on the chunks' slots.
+template <int C>
+__device__ __forceinline__ int64_t first_segment(const DeltaArgs &p, int64_t n, int64_t t0)
+{
+    const int64_t each = (p.tokens + C - 1) / C;
+    return p.offsets ? first_slot<C>(p, n, t0) / p.seg + n : n * (each > 0 ? (each + p.seg - 1) / p.seg : 1);
+}
+// The sequence of a segment's slot (slots between two sequences' belong to the one before).
+template <int C>
+__device__ __forceinline__ int64_t segment_sequence(const DeltaArgs &p, int64_t sg)
+{
+    int64_t lo = 0, hi = p.batch - 1, t0, all;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) / 2;
+        sequence(p, mid, t0, all);
+        if (first_segment<C>(p, mid, t0) <= sg)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
 }
 
 // 2^x for x <= 0 in 64 bits: the whole part by the exponent, so that a large x costs no precision
