@@ -522,12 +522,14 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     }
 }
 
-// From the state before a segment to the one after it, M S + N, over a sequence's segments: 16 columns of one head a wavefront.
+// From the state before a segment to the one after it, M S + N, over a sequence's segments: 16 columns of one head a block, 32 rows of the state a wavefront, its rows of
+// M loaded a segment ahead.
 template <int C, int DKP>
-__global__ __launch_bounds__(64) void k_delta_join(DeltaArgs p)
+__global__ __launch_bounds__(2 * DKP) void k_delta_join(DeltaArgs p)
 {
-    constexpr int KT = DKP / 16, KS = DKP / 32;
-    const int lane = threadIdx.x, col = lane & 15, x4 = lane >> 4, slices = p.dvp / 16;
+    constexpr int KS = DKP / 32;
+    __shared__ __align__(16) char state[2][KS * NX * UNIT];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, x4 = lane >> 4, slices = p.dvp / 16;
     const int c0 = (int)(blockIdx.x % slices) * 16 + col, h = blockIdx.x / slices % p.hv;
     const int64_t n = blockIdx.x / slices / p.hv;
     int64_t t0, len;
@@ -536,37 +538,58 @@ __global__ __launch_bounds__(64) void k_delta_join(DeltaArgs p)
     const int parts = (int)((len + (int64_t)C * p.seg - 1) / ((int64_t)C * p.seg));
     if (parts < 3)
         return;  // (the state before segment 1 is there)
-    f32x4 S[KT];
-    auto at = [&](int64_t g) { return in_memory(p.seg_state + ((g * p.hv + h) * DKP) * (int64_t)p.dvp + c0); };
+    f32x4 S[2], N[2];
+    f32x8 m[2][KS];
+    auto at = [&](int64_t g) { return p.seg_state + ((g * p.hv + h) * DKP) * (int64_t)p.dvp + c0; };
+    auto rows_of = [&](int64_t g, f32x4 *x) {
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            S[i][r] = at(sg + 1)[(int64_t)(first_of(i) + r) * p.dvp];
-    for (int g = 1; g + 1 < parts; ++g) {
-        const float *M = p.seg_map + ((sg + g) * p.hv + h) * DKP * (int64_t)DKP;
-        Frag<NX> f[KS];
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-            f[s] = split<NX>(join(S[2 * s], S[2 * s + 1]));
-#pragma unroll
-        for (int i = 0; i < KT; ++i) {
-            f32x8 m[KS];
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                m[s] = load8<float>(M + element_of(i, col) * DKP + 32 * s + 8 * x4, 8);
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                S[i][r] = at(sg + g + 1)[(int64_t)(first_of(i) + r) * p.dvp];
+                x[i][r] = in_memory(at(g))[(int64_t)(first_of(2 * wave + i) + r) * p.dvp];
+    };
+    auto map_of = [&](int64_t g) {
+        const float *M = p.seg_map + (g * p.hv + h) * DKP * (int64_t)DKP;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int s = 0; s < KS; ++s)
-                mma<3>(S[i], split<NX>(m[s]), f[s]);
+                m[i][s] = load8<float>(M + element_of(2 * wave + i, col) * DKP + 32 * s + 8 * x4, 8);
+    };
+    rows_of(sg + 1, S);
+    map_of(sg + 1);
+    rows_of(sg + 2, N);
+    for (int g = 1; g + 1 < parts; ++g) {
+        char *buf = state[g & 1];
+        const Frag<NX> own = split<NX>(join(S[0], S[1]));
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+            *reinterpret_cast<bf16x8 *>(buf + (wave * NX + i) * UNIT + 16 * lane) = own.p[i];
+        Frag<NX> f[2][KS];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            S[i] = N[i];
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                f[i][s] = split<NX>(m[i][s]);
+        }
+        if (g + 2 < parts) {
+            map_of(sg + g + 1);
+            rows_of(sg + g + 2, N);
+        }
+        block_barrier();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const Frag<NX> x = unit<NX>(buf, s * NX, 1);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                mma<3>(S[i], f[i][s], x);
         }
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                at(sg + g + 1)[(int64_t)(first_of(i) + r) * p.dvp] = S[i][r];
+                in_memory(at(sg + g + 1))[(int64_t)(first_of(2 * wave + i) + r) * p.dvp] = S[i][r];
     }
 }
 
@@ -579,7 +602,7 @@ static la_status scan_s(DeltaArgs &p, hipStream_t st)
     if (p.seg) {
         p.slices = vslices + (p.dk + 63) / 64;
         LA_LAUNCH((k_delta_scan<T, DKP, SAVE, true>), dim3((unsigned)(p.segs * p.hv * p.slices)), dim3(512), 0, st, p);
-        LA_LAUNCH((k_delta_join<Pack<T, DKP>::C, DKP>), dim3((unsigned)(p.batch * p.hv * (p.dvp / 16))), dim3(64), 0, st, p);
+        LA_LAUNCH((k_delta_join<Pack<T, DKP>::C, DKP>), dim3((unsigned)(p.batch * p.hv * (p.dvp / 16))), dim3(2 * DKP), 0, st, p);
     }
     p.slices = vslices;
     LA_LAUNCH((k_delta_scan<T, DKP, SAVE, false>), dim3((unsigned)((p.seg ? p.segs : p.batch) * p.hv * p.slices)), dim3(512), 0, st, p);

@@ -99,6 +99,22 @@ __device__ __forceinline__ void store_part(T *p, int n, const acc_of<T> (&v)[N])
     }
 }
 
+// as they are in memory, zeros past `n`
+template <typename T, int N>
+__device__ __forceinline__ typename PackOf<T, N>::whole load_raw(const T *p, int n)
+{
+    typename PackOf<T, N>::whole x;
+    if (n >= N) {
+        x = *(typename PackOf<T, N>::source)p;
+    } else {
+        p = opaque(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            x[i] = i < n ? in_memory(p)[i] : (T)0;
+    }
+    return x;
+}
+
 template <typename A>
 __device__ __forceinline__ A wave_sum(A x)
 {
@@ -108,6 +124,5 @@ __device__ __forceinline__ A wave_sum(A x)
     return x;
 }
 
-inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace la

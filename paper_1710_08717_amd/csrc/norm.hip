@@ -49,26 +49,27 @@ __device__ __forceinline__ void row_sums(A &a, A &b, int turn)
     }
 }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void load_weight(const void *w, int w32, int64_t col, acc_of<T> (&v)[VEC])
+// N elements of the weight or the bias, those past `n` as zeros
+template <typename T, int N>
+__device__ __forceinline__ void load_weight(const void *w, int w32, int col, int n, acc_of<T> (&v)[N])
 {
     if (sizeof(T) == 2 && w32) {
-        float f[VEC];
-        load_pack<float, VEC>((const float *)w + col, f);
+        float f[N];
+        load_part<float, N>((const float *)w + col, n, f);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
+        for (int i = 0; i < N; ++i)
             v[i] = f[i];
     } else {
-        load_pack<T, VEC>((const T *)w + col, v);
+        load_part<T, N>((const T *)w + col, n, v);
     }
 }
 
-// TPR lanes a row, R packs of VEC elements a lane.  A column past n only arises in whole packs: VEC divides n.
-template <typename T, int VEC, int TPR, int R>
+// TPR lanes a row, R packs of 16 bytes a lane; the row's last pack may be a part of one, and rows may start anywhere.
+template <typename T, int TPR, int R>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm(NormArgs p)
 {
     using A = acc_of<T>;
-    constexpr int NT = TPR < 256 ? 256 : TPR;
+    constexpr int NT = TPR < 256 ? 256 : TPR, VEC = 16 / sizeof(T);
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     if (row >= p.rows)
@@ -79,13 +80,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm(NormArgs p
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int col = (r * TPR + lane) * VEC;
-        if (col < p.n) {
-            load_pack<T, VEC>(x + col, v[r]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                v[r][i] = 0;
-        }
+        load_part<T, VEC>(x + col, p.n - col, v[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -96,14 +91,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm(NormArgs p
     const A mean = sum / p.n;
     A sq = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if ((r * TPR + lane) * VEC < p.n) {
+    for (int r = 0; r < R; ++r) {
+        const int left = p.n - (r * TPR + lane) * VEC;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const A d = v[r][i] - mean;
-                sq += d * d;
-            }
+        for (int i = 0; i < VEC; ++i) {
+            const A d = i < left ? v[r][i] - mean : A(0);
+            sq += d * d;
         }
+    }
     row_sums<TPR>(sq, none, 1);
     const A rstd = A(1) / sqrt(sq / p.n + (A)p.eps);
     if (lane == 0 && p.mean) {
@@ -112,8 +107,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm(NormArgs p
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int col = (r * TPR + lane) * VEC;
-        if (col < p.n) {
+        const int col = (r * TPR + lane) * VEC, left = p.n - col;
+        if (left > 0) {
             A w[VEC], c[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
@@ -121,23 +116,24 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm(NormArgs p
                 c[i] = 0;
             }
             if (p.w)
-                load_weight<T, VEC>(p.w, p.w32, col, w);
+                load_weight<T, VEC>(p.w, p.w32, col, left, w);
             if (p.c)
-                load_weight<T, VEC>(p.c, p.w32, col, c);
+                load_weight<T, VEC>(p.c, p.w32, col, left, c);
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
                 v[r][i] = (v[r][i] - mean) * rstd * w[i] + c[i];
-            store_pack<T, VEC>(y + col, v[r]);
+            store_part<T, VEC>(y + col, left, v[r]);
         }
     }
 }
 
-// A block takes every gridDim.x-th group of rows and keeps its part of w_bar and c_bar in registers: a lane's columns are the same in every row.
-template <typename T, int VEC, int TPR, int R>
+// A block takes every gridDim.x-th group of rows and keeps its part of w_bar and c_bar in registers: a lane's columns are the same in every row.  The next
+// row is loaded before this one's sums are joined.
+template <typename T, int TPR, int R>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm_back(NormArgs p)
 {
     using A = acc_of<T>;
-    constexpr int NT = TPR < 256 ? 256 : TPR, GROUPS = NT / TPR;
+    constexpr int NT = TPR < 256 ? 256 : TPR, GROUPS = NT / TPR, VEC = 16 / sizeof(T);
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const A inv_n = A(1) / p.n;
     A w[R][VEC], wb[R][VEC], cb[R][VEC];
@@ -149,34 +145,43 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm_back(NormA
             w[r][i] = 1;
             wb[r][i] = cb[r][i] = 0;
         }
-        if (p.w && col < p.n)
-            load_weight<T, VEC>(p.w, p.w32, col, w[r]);
+        if (p.w)
+            load_weight<T, VEC>(p.w, p.w32, col, p.n - col, w[r]);
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < p.rows; row += (int64_t)gridDim.x * GROUPS, turn ^= 1) {
+    typename PackOf<T, VEC>::whole xr[R], yr[R];
+    A mean = 0, rstd = 0;
+    auto fetch = [&](int64_t row) {
         const T *x = (const T *)p.x + row * p.ldx, *yb = (const T *)p.yb + row * p.n;
-        const A mean = ((const A *)p.mean)[row], rstd = ((const A *)p.rstd)[row];
-        A h[R][VEC], g[R][VEC];
+        mean = ((const A *)p.mean)[row];
+        rstd = ((const A *)p.rstd)[row];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int col = (r * TPR + lane) * VEC;
-            if (col < p.n) {
-                load_pack<T, VEC>(x + col, h[r]);
-                load_pack<T, VEC>(yb + col, g[r]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    h[r][i] = mean;
-                    g[r][i] = 0;
-                }
-            }
+            xr[r] = load_raw<T, VEC>(x + col, p.n - col);
+            yr[r] = load_raw<T, VEC>(yb + col, p.n - col);
         }
-        A s = 0, q = 0;
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+    if (row < p.rows)
+        fetch(row);
+    int turn = 0;
+    for (; row < p.rows; row += step, turn ^= 1) {
+        A h[R][VEC], g[R][VEC], s = 0, q = 0;
+        const A scale = rstd;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {  // (past the row's end y_bar is zero)
+                h[r][i] = ((A)xr[r][i] - mean) * scale;
+                g[r][i] = (A)yr[r][i];
+            }
+        if (row + step < p.rows)
+            fetch(row + step);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                h[r][i] = (h[r][i] - mean) * rstd;
                 wb[r][i] += g[r][i] * h[r][i];
                 cb[r][i] += g[r][i];
                 g[r][i] *= w[r][i];
@@ -191,9 +196,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm_back(NormA
             const int col = (r * TPR + lane) * VEC;
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
-                g[r][i] = rstd * (g[r][i] - s - h[r][i] * q);
-            if (col < p.n)
-                store_pack<T, VEC>((T *)p.y + row * p.n + col, g[r]);
+                g[r][i] = scale * (g[r][i] - s - h[r][i] * q);
+            store_part<T, VEC>((T *)p.y + row * p.n + col, p.n - col, g[r]);
         }
     }
     A *part = (A *)p.part + (int64_t)blockIdx.x * 2 * p.n;
@@ -222,13 +226,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm_back(NormA
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int col = (r * TPR + lane) * VEC;
-        if (col < p.n) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                part[col + i] = wb[r][i];
-                part[p.n + col + i] = cb[r][i];
-            }
-        }
+        store_part<A, VEC>(part + col, p.n - col, wb[r]);
+        store_part<A, VEC>(part + p.n + col, p.n - col, cb[r]);
     }
 }
 
@@ -288,9 +287,9 @@ __global__ __launch_bounds__(1024) void k_layer_norm_wide(NormArgs p)
     for (int i = threadIdx.x; i < p.n; i += 1024) {
         A w[1] = {1}, c[1] = {0};
         if (p.w)
-            load_weight<T, 1>(p.w, p.w32, i, w);
+            load_weight<T, 1>(p.w, p.w32, i, 1, w);
         if (p.c)
-            load_weight<T, 1>(p.c, p.w32, i, c);
+            load_weight<T, 1>(p.c, p.w32, i, 1, c);
         ((T *)p.y)[row * p.n + i] = (T)(((A)x[i] - mean) * rstd * w[0] + c[0]);
     }
 }
@@ -306,7 +305,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_back_wide(NormArgs p)
     for (int i = threadIdx.x; i < p.n; i += 1024) {
         A w[1] = {1};
         if (p.w)
-            load_weight<T, 1>(p.w, p.w32, i, w);
+            load_weight<T, 1>(p.w, p.w32, i, 1, w);
         const A t = (A)yb[i] * w[0];
         s += t;
         q += t * (((A)x[i] - mean) * rstd);
@@ -317,7 +316,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_back_wide(NormArgs p)
     for (int i = threadIdx.x; i < p.n; i += 1024) {
         A w[1] = {1};
         if (p.w)
-            load_weight<T, 1>(p.w, p.w32, i, w);
+            load_weight<T, 1>(p.w, p.w32, i, 1, w);
         const A h = ((A)x[i] - mean) * rstd;
         ((T *)p.y)[row * p.n + i] = (T)(rstd * ((A)yb[i] * w[0] - s - h * q));
     }
@@ -369,7 +368,7 @@ static NormShape norm_shape(int n, int vec, int64_t rows)
     return {0, 0};
 }
 
-constexpr int NORM_BLOCKS = 512;
+constexpr int NORM_BLOCKS = 1024;
 
 // blocks of the gradient's kernel: each keeps 2 n sums, written and read once
 static int norm_blocks(int64_t rows, NormShape s)
@@ -379,49 +378,43 @@ static int norm_blocks(int64_t rows, NormShape s)
     return (int)(want < NORM_BLOCKS ? want : NORM_BLOCKS);
 }
 
-template <typename T, int VEC, int TPR, int R>
+template <typename T, int TPR, int R>
 static void norm_launch(const NormArgs &p, bool back, hipStream_t st)
 {
     constexpr int NT = TPR < 256 ? 256 : TPR, GROUPS = NT / TPR;
     if (back)
-        LA_LAUNCH((k_layer_norm_back<T, VEC, TPR, R>), dim3(norm_blocks(p.rows, {TPR, R})), dim3(NT), 0, st, p);
+        LA_LAUNCH((k_layer_norm_back<T, TPR, R>), dim3(norm_blocks(p.rows, {TPR, R})), dim3(NT), 0, st, p);
     else
-        LA_LAUNCH((k_layer_norm<T, VEC, TPR, R>), dim3((unsigned)((p.rows + GROUPS - 1) / GROUPS)), dim3(NT), 0, st, p);
+        LA_LAUNCH((k_layer_norm<T, TPR, R>), dim3((unsigned)((p.rows + GROUPS - 1) / GROUPS)), dim3(NT), 0, st, p);
 }
 
-template <typename T, int VEC>
+template <typename T>
 static void norm_dispatch(const NormArgs &p, NormShape s, bool back, hipStream_t st)
 {
     if (s.tpr == 64 && s.r == 1)
-        norm_launch<T, VEC, 64, 1>(p, back, st);
+        norm_launch<T, 64, 1>(p, back, st);
     else if (s.tpr == 64)
-        norm_launch<T, VEC, 64, 2>(p, back, st);
+        norm_launch<T, 64, 2>(p, back, st);
     else if (s.tpr == 256 && s.r == 1)
-        norm_launch<T, VEC, 256, 1>(p, back, st);
+        norm_launch<T, 256, 1>(p, back, st);
     else if (s.tpr == 256 && s.r == 2)
-        norm_launch<T, VEC, 256, 2>(p, back, st);
+        norm_launch<T, 256, 2>(p, back, st);
     else if (s.tpr == 256)
-        norm_launch<T, VEC, 256, 4>(p, back, st);
+        norm_launch<T, 256, 4>(p, back, st);
     else if (s.r == 2)
-        norm_launch<T, VEC, 1024, 2>(p, back, st);
+        norm_launch<T, 1024, 2>(p, back, st);
     else
-        norm_launch<T, VEC, 1024, 4>(p, back, st);
+        norm_launch<T, 1024, 4>(p, back, st);
 }
 
 template <typename T>
 static la_status norm_t(const NormArgs &p, bool back, void *wb, void *cb, int wtype, hipStream_t st)
 {
     using A = acc_of<T>;
-    constexpr int VEC = 16 / sizeof(T);
-    // whole packs of 16 bytes where every row starts on one (weight and bias in 32 bits: two packs of them)
-    const bool packs = p.n % VEC == 0 && p.ldx % VEC == 0 && aligned16(p.x) && aligned16(p.y) && aligned16(p.yb) && aligned16(p.w) && aligned16(p.c);
-    const NormShape s = norm_shape(p.n, packs ? VEC : 1, p.rows);
+    const NormShape s = norm_shape(p.n, 16 / sizeof(T), p.rows);
     int parts = norm_blocks(p.rows, s);
     if (s.tpr) {
-        if (packs)
-            norm_dispatch<T, VEC>(p, s, back, st);
-        else
-            norm_dispatch<T, 1>(p, s, back, st);
+        norm_dispatch<T>(p, s, back, st);
     } else if (!back) {
         LA_LAUNCH((k_layer_norm_wide<T>), dim3((unsigned)p.rows), dim3(1024), 0, st, p);
     } else {
