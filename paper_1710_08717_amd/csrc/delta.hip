@@ -241,38 +241,39 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 // ---------------------------------------------------------------------------------
 // the walk over a sequence's chunks
 // ---------------------------------------------------------------------------------
-// A block takes 64 columns of V: four groups of 16, two wavefronts each.  A wavefront sums K S and Q S over its half of the state's rows, for all tokens, takes
+// A block takes NG groups of 16 columns of V, two wavefronts each.  A wavefront sums K S and Q S over its half of the state's rows, for all tokens, takes
 // the other half's sums for its half of the tokens, forms Z, U and the answers of those, and with everybody's U its half of the new state.  The packets of
 // the next chunk come straight to LDS, into the place of this one's as soon as all have read them.
 //
 // Where sequences and heads are too few to fill the chip, a sequence is walked in segments side by side.  The state after a segment is M S + N with S the state
 // before it: MAP blocks find N (the walk from a state of zeros) and the columns of M (from the unit vectors, with V zero), without answers;
 // k_delta_join goes from segment to segment; then every segment is walked from its own state.
-template <typename T, int DKP, bool SAVE, bool MAP>
-__global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
+template <typename T, int DKP, int NG, bool SAVE, bool MAP>
+__global__ __launch_bounds__(128 * NG) void k_delta_scan(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = 4;  // NL wavefronts load the packets: those of the first half, which have less to do with T
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = NG;  // NL wavefronts load the packets: those of the first half, which have less to do with T
     constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;  // a wavefront's tiles of tokens and of the state, steps over the state
     constexpr int LQ = NI * FK, LP = NX * FT;
     constexpr int NKQ = (MAP ? 1 : 2) * NI * FK, NTP = (MAP ? NX : NX + G::NO) * FT;
     constexpr int EACH_KQ = share<NKQ, NL>(), EACH_TP = share<NTP, NL>() + 1, EACH_KT = share<NI * FK, NL>();
-    using In = RowsIn<T, C, 4, 512>;
+    using In = RowsIn<T, C, NG, 128 * NG>;
     constexpr int EX1 = 4 * HT * UNIT > CS * NX * UNIT ? 4 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its U
     constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's Z; then rows on their way out
     __shared__ __align__(16) char kq[NKQ * UNIT];
     __shared__ __align__(16) char tp[NTP * UNIT];
     __shared__ __align__(16) char decays[2][UNIT];
     __shared__ __align__(16) char turned[NI * FK * UNIT];
-    __shared__ __align__(16) char vin[C * 64 * sizeof(T)];
-    __shared__ __align__(16) char ex1_all[4][EX1], ex2_all[4][EX2];
+    __shared__ __align__(16) char vin[C * 16 * NG * sizeof(T)];
+    __shared__ __align__(16) char ex1_all[NG][EX1], ex2_all[NG][EX2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
-    const int half = wave >> 2, set = wave & 3;
-    const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
-    const int64_t sg = blockIdx.x / p.slices / p.hv, n = p.seg ? segment_sequence<C>(p, sg) : sg;
-    const int vslices = (p.dv + 63) / 64;
+    const int half = wave / NG, set = wave % NG;
+    const unsigned block = block_of_die(p.slices);
+    const int slice = block % p.slices, h = block / p.slices % p.hv;
+    const int64_t sg = block / p.slices / p.hv, n = p.seg ? segment_sequence<C>(p, sg) : sg;
+    const int vslices = (p.dv + 16 * NG - 1) / (16 * NG);
     const bool unit_columns = MAP && slice >= vslices;
-    const int sbase = (unit_columns ? slice - vslices : slice) * 64, cbase = sbase + set * 16, c0 = cbase + col;  // this lane's column of V (or of M)
+    const int sbase = (unit_columns ? slice - vslices : slice) * 16 * NG, cbase = sbase + set * 16, c0 = cbase + col;  // this lane's column of V (or of M)
     const int width = unit_columns ? p.dk : p.dv;
     const bool live = c0 < width, kept = cbase < p.dvp;
     int64_t t0, len;
@@ -299,9 +300,9 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
     const char *pk = p.pack_k + (slot0 * p.hk + hk) * (int64_t)(G::key_units(SAVE) * UNIT), *pv = p.pack_v + (slot0 * p.hv + h) * (int64_t)(G::value_units(SAVE) * UNIT);
     const int64_t key_step = (int64_t)p.hk * (G::key_units(SAVE) * UNIT), value_step = (int64_t)p.hv * (G::value_units(SAVE) * UNIT);
     const uint32_t kq_at = lds_address(kq), tp_at = lds_address(tp), turned_at = lds_address(turned), decays_at = lds_address(decays);
-    auto fetch_kq = [&](const char *k) { stream_run<NKQ, NL>(k, kq_at, wave); };
+    auto fetch_kq = [&](const char *k) { stream_run<NKQ, NL>(k, kq_at, set); };
     auto fetch_tp = [&](const char *v, int buffer) {
-        stream_run<NTP, NL>(v + G::TINV * UNIT, tp_at, wave);
+        stream_run<NTP, NL>(v + G::TINV * UNIT, tp_at, set);
         stream_units<1>(v + UNIT, decays_at + buffer * UNIT);  // (by each of them)
     };
     char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(DeltaArgs p)
         const bool more = c + 1 < chunks;
         block_barrier();  // K, Q and V are there, all have read what the chunk before left
         if (!half)
-            stream_run<NI * FK, NL>(pk + G::KTURN * UNIT, turned_at, wave);
+            stream_run<NI * FK, NL>(pk + G::KTURN * UNIT, turned_at, set);
         f32x4 X[RT], Y[RT], U[HT], in[HT], out[HT], beta[HT];
 #pragma unroll
         for (int i = 0; i < RT; ++i)
@@ -593,19 +594,28 @@ __global__ __launch_bounds__(2 * DKP) void k_delta_join(DeltaArgs p)
     }
 }
 
+template <typename T, int DKP, int NG, bool SAVE>
+static void walk(DeltaArgs &p, hipStream_t st)
+{
+    const int vslices = (p.dv + 16 * NG - 1) / (16 * NG);
+    if (p.seg) {
+        p.slices = vslices + (p.dk + 16 * NG - 1) / (16 * NG);
+        LA_LAUNCH((k_delta_scan<T, DKP, NG, SAVE, true>), dim3((unsigned)(p.segs * p.hv * p.slices)), dim3(128 * NG), 0, st, p);
+        LA_LAUNCH((k_delta_join<Pack<T, DKP>::C, DKP>), dim3((unsigned)(p.batch * p.hv * (p.dvp / 16))), dim3(2 * DKP), 0, st, p);
+    }
+    p.slices = vslices;
+    LA_LAUNCH((k_delta_scan<T, DKP, NG, SAVE, false>), dim3((unsigned)((p.seg ? p.segs : p.batch) * p.hv * p.slices)), dim3(128 * NG), 0, st, p);
+}
+
 template <typename T, int DKP, bool SAVE>
 static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
     if (p.slots > 0)
         LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
-    const int vslices = (p.dv + 63) / 64;
-    if (p.seg) {
-        p.slices = vslices + (p.dk + 63) / 64;
-        LA_LAUNCH((k_delta_scan<T, DKP, SAVE, true>), dim3((unsigned)(p.segs * p.hv * p.slices)), dim3(512), 0, st, p);
-        LA_LAUNCH((k_delta_join<Pack<T, DKP>::C, DKP>), dim3((unsigned)(p.batch * p.hv * (p.dvp / 16))), dim3(2 * DKP), 0, st, p);
-    }
-    p.slices = vslices;
-    LA_LAUNCH((k_delta_scan<T, DKP, SAVE, false>), dim3((unsigned)((p.seg ? p.segs : p.batch) * p.hv * p.slices)), dim3(512), 0, st, p);
+    if (walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2)
+        walk<T, DKP, 2, SAVE>(p, st);
+    else
+        walk<T, DKP, 4, SAVE>(p, st);
     return launch_check("delta rule");
 }
 template <typename T, int DKP>

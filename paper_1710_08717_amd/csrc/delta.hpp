@@ -122,6 +122,18 @@ __device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shuff
 __device__ __forceinline__ int element_of(int i, int m) { return 32 * (i >> 1) + 8 * (m >> 2) + 4 * (i & 1) + (m & 3); }
 __device__ __forceinline__ int first_of(int i) { return 32 * (i >> 1) + 8 * ((threadIdx.x & 63) >> 4) + 4 * (i & 1); }
 
+// Block b runs on die b % 8 of the 8: an order in which the `slices` blocks of a head, which read the same packets, run on the same die and find them in its
+// cache, while the heads go round the dies (sequences of like lengths may lie side by side).
+__device__ __forceinline__ unsigned block_of_die(unsigned slices)
+{
+    const unsigned b = blockIdx.x, whole = gridDim.x / slices / 8 * 8 * slices, i = b / 8;
+    return b < whole ? (i / slices * 8 + b % 8) * slices + i % slices : b;
+}
+
+// Column groups of 16 of a walk's block: two where four would leave half of the compute units idle.  A block of two has a SIMD for every wavefront, and a chunk takes
+// it less time; with more blocks than compute units four groups share what they load (2 x 4096 tokens, 32 heads of 128, bf16: %NG%).
+inline int walk_groups(int64_t heads, int dv) { return heads * ((dv + 63) / 64) * 2 <= 256 ? 2 : 4; }
+
 // Two wavefronts share 16 columns of a walk: wavefront `half` keeps the state's rows and forms the chunk's tokens of its half of the tiles.  What the other one
 // needs of it passes through LDS: operands of a step (32 tokens), whose tiles a wavefront has both (RT = 4, step `half`) or one of (RT = 2).
 template <int RT>

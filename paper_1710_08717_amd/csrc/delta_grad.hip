@@ -20,28 +20,29 @@
 namespace la {
 
 // Wavefronts as in the forward walk: the sums of K S1_bar in halves, U_bar and Z_bar of a half of the tokens, a half of the new gradient of the state.
-template <typename T, int DKP>
-__global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
+template <typename T, int DKP, int NG>
+__global__ __launch_bounds__(128 * NG) void k_delta_scan_back(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
-    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = 4;  // NL wavefronts load the packets: those of the second half, which have less to do with T^T
+    constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FK = G::FK, FT = G::FT, NL = NG;  // NL wavefronts load the packets: those of the second half, which have less to do with T^T
     constexpr int HT = RT / 2, HK = G::KT / 2, HS = G::KS / 2;
     constexpr int LQ = NI * FK, LP = NX * FT;
     constexpr int EACH_K = share<NI * FK, NL>() + 1, EACH_TP = 2 * share<NX * FT, NL>(), EACH_KT = share<2 * NI * FK, NL>();
-    using In = RowsIn<T, C, 4, 512>;
+    using In = RowsIn<T, C, NG, 128 * NG>;
     constexpr int EX1 = 2 * HT * UNIT > CS * NX * UNIT ? 2 * HT * UNIT : CS * NX * UNIT;                                // a group's sums; then its X_bar
     constexpr int EX2 = CS * NX * UNIT > 2 * rows_out_bytes<HT>() ? CS * NX * UNIT : 2 * rows_out_bytes<HT>();  // a group's U_bar; then rows on their way out
     __shared__ __align__(16) char keys[NI * FK * UNIT];
     __shared__ __align__(16) char tp[2 * NX * FT * UNIT];  // T^T and P^T
     __shared__ __align__(16) char decays[2][UNIT];
     __shared__ __align__(16) char turned[2 * NI * FK * UNIT];  // Kt and Qt
-    __shared__ __align__(16) char oin[C * 64 * sizeof(T)];
-    __shared__ __align__(16) char ex1_all[4][EX1], ex2_all[4][EX2];
+    __shared__ __align__(16) char oin[C * 16 * NG * sizeof(T)];
+    __shared__ __align__(16) char ex1_all[NG][EX1], ex2_all[NG][EX2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
-    const int half = wave >> 2, set = wave & 3;
-    const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv;
-    const int64_t n = blockIdx.x / p.slices / p.hv;
-    const int cbase = slice * 64 + set * 16, c0 = cbase + col;
+    const int half = wave / NG, set = wave % NG;
+    const unsigned block = block_of_die(p.slices);
+    const int slice = block % p.slices, h = block / p.slices % p.hv;
+    const int64_t n = block / p.slices / p.hv;
+    const int cbase = slice * 16 * NG + set * 16, c0 = cbase + col;
     const bool live = c0 < p.dv, kept = cbase < p.dvp;
     int64_t t0, len;
     sequence(p, n, t0, len);
@@ -64,8 +65,8 @@ __global__ __launch_bounds__(512) void k_delta_scan_back(DeltaArgs p)
     char *ex1 = ex1_all[set], *ex2 = ex2_all[set], *mine = ex2 + half * rows_out_bytes<HT>();
     In O;
     auto fetch_o = [&](int c) {
-        O.fetch((const T *)p.o_bar + ((t0 + (int64_t)c * C) * p.hv + h) * p.dv + slice * 64, ldo, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
-                p.dv - slice * 64);
+        O.fetch((const T *)p.o_bar + ((t0 + (int64_t)c * C) * p.hv + h) * p.dv + slice * 16 * NG, ldo, (int)(len - (int64_t)c * C < C ? len - (int64_t)c * C : C),
+                p.dv - slice * 16 * NG);
     };
     auto keep_state = [&](int c, const f32x4 *S) {
         if (kept) {
@@ -601,8 +602,13 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 template <typename T, int DKP>
 static la_status back_t(DeltaArgs &p, hipStream_t st)
 {
-    p.slices = (p.dv + 63) / 64;
-    LA_LAUNCH((k_delta_scan_back<T, DKP>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
+    if (walk_groups(p.batch * p.hv, p.dv) == 2) {
+        p.slices = (p.dv + 31) / 32;
+        LA_LAUNCH((k_delta_scan_back<T, DKP, 2>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(256), 0, st, p);
+    } else {
+        p.slices = (p.dv + 63) / 64;
+        LA_LAUNCH((k_delta_scan_back<T, DKP, 4>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
+    }
     if (p.slots > 0)
         LA_LAUNCH((k_delta_grads<T, DKP>), dim3((unsigned)(p.slots * p.hk)), dim3(4 * DKP), 0, st, p);
     return launch_check("delta rule backward");

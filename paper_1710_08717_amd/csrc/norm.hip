@@ -231,11 +231,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layer_norm_back(NormA
     }
 }
 
-// w_bar and c_bar from the blocks' parts: 32 columns a block, 8 runs of parts side by side, joined in their order
+// w_bar and c_bar from the blocks' parts: 32 columns a block, 32 runs of parts side by side, joined in their order
 template <typename A>
-__global__ __launch_bounds__(256) void k_norm_parts(const A *part, int parts, int n, void *wb, void *cb, int type)
+__global__ __launch_bounds__(1024) void k_norm_parts(const A *part, int parts, int n, void *wb, void *cb, int type)
 {
-    __shared__ A box[8][33];
+    __shared__ A box[32][33];
     const int c = threadIdx.x % 32, run = threadIdx.x / 32, col = blockIdx.x * 32 + c;
     void *out = blockIdx.y ? cb : wb;
     if (!out)
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(256) void k_norm_parts(const A *part, int parts, in
     if (col < n) {
         const A *p = part + (int64_t)blockIdx.y * n + col;
 #pragma unroll 8
-        for (int i = run; i < parts; i += 8)
+        for (int i = run; i < parts; i += 32)
             s += p[(int64_t)i * 2 * n];
     }
     box[run][c] = s;
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void k_norm_parts(const A *part, int parts, in
     if (run || col >= n)
         return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k)
+    for (int k = 1; k < 32; ++k)
         s += box[k][c];
     if (type == LA_BF16)
         ((bf16_t *)out)[col] = (bf16_t)s;
@@ -348,8 +348,9 @@ __global__ __launch_bounds__(256) void k_norm_columns_wide(NormArgs p)
 struct NormShape {
     int tpr, r;
 };
-static NormShape norm_shape(int n, int vec, int64_t rows)
+static NormShape norm_shape(int n, int size, int64_t rows, bool back)
 {
+    const int vec = 16 / size;
     const int packs = (n + vec - 1) / vec;
     if (packs <= 64)
         return {64, 1};
@@ -361,31 +362,36 @@ static NormShape norm_shape(int n, int vec, int64_t rows)
         return {256, 2};
     if (packs <= 1024)
         return {256, 4};
+    // (the gradient holds five numbers for each of a lane's columns: 8 of 16 bits do not fit four times into what 1024 lanes leave each)
     if (packs <= 2048)
-        return {1024, 2};
-    if (packs <= 4096)
+        return back ? NormShape{512, 4} : NormShape{1024, 2};
+    if (packs <= 4096 && !(back && size == 2))
         return {1024, 4};
     return {0, 0};
 }
 
 constexpr int NORM_BLOCKS = 1024;
 
-// blocks of the gradient's kernel: each keeps 2 n sums, written and read once
+// Blocks of the gradient's kernel: enough to fill the chip, but 4 rows at least to each, since a block's 2 n sums are written and read once.
 static int norm_blocks(int64_t rows, NormShape s)
 {
     const int groups = s.tpr && s.tpr < 256 ? 256 / s.tpr : 1;
-    const int64_t want = s.tpr ? (rows + groups - 1) / groups : (rows < 64 ? rows : 64);
-    return (int)(want < NORM_BLOCKS ? want : NORM_BLOCKS);
+    const int64_t all = (rows + groups - 1) / groups, most = rows / 4 < 256 ? 256 : rows / 4 < NORM_BLOCKS ? rows / 4 : NORM_BLOCKS;
+    return (int)(s.tpr == 0 ? (rows < 64 ? rows : 64) : all < most ? all : most);
 }
 
 template <typename T, int TPR, int R>
 static void norm_launch(const NormArgs &p, bool back, hipStream_t st)
 {
     constexpr int NT = TPR < 256 ? 256 : TPR, GROUPS = NT / TPR;
-    if (back)
-        LA_LAUNCH((k_layer_norm_back<T, TPR, R>), dim3(norm_blocks(p.rows, {TPR, R})), dim3(NT), 0, st, p);
-    else
-        LA_LAUNCH((k_layer_norm<T, TPR, R>), dim3((unsigned)((p.rows + GROUPS - 1) / GROUPS)), dim3(NT), 0, st, p);
+    // (what norm_shape gives for one of the two only)
+    constexpr bool FORWARD = TPR != 512, BACK = !(TPR == 1024 && (R == 2 || sizeof(T) == 2));
+    if constexpr (BACK)
+        if (back)
+            LA_LAUNCH((k_layer_norm_back<T, TPR, R>), dim3(norm_blocks(p.rows, {TPR, R})), dim3(NT), 0, st, p);
+    if constexpr (FORWARD)
+        if (!back)
+            LA_LAUNCH((k_layer_norm<T, TPR, R>), dim3((unsigned)((p.rows + GROUPS - 1) / GROUPS)), dim3(NT), 0, st, p);
 }
 
 template <typename T>
@@ -401,6 +407,8 @@ static void norm_dispatch(const NormArgs &p, NormShape s, bool back, hipStream_t
         norm_launch<T, 256, 2>(p, back, st);
     else if (s.tpr == 256)
         norm_launch<T, 256, 4>(p, back, st);
+    else if (s.tpr == 512)
+        norm_launch<T, 512, 4>(p, back, st);
     else if (s.r == 2)
         norm_launch<T, 1024, 2>(p, back, st);
     else
@@ -411,7 +419,7 @@ template <typename T>
 static la_status norm_t(const NormArgs &p, bool back, void *wb, void *cb, int wtype, hipStream_t st)
 {
     using A = acc_of<T>;
-    const NormShape s = norm_shape(p.n, 16 / sizeof(T), p.rows);
+    const NormShape s = norm_shape(p.n, sizeof(T), p.rows, back);
     int parts = norm_blocks(p.rows, s);
     if (s.tpr) {
         norm_dispatch<T>(p, s, back, st);
@@ -423,7 +431,7 @@ static la_status norm_t(const NormArgs &p, bool back, void *wb, void *cb, int wt
         LA_LAUNCH((k_layer_norm_back_wide<T>), dim3((unsigned)p.rows), dim3(1024), 0, st, p);
     }
     if (back && (wb || cb))
-        LA_LAUNCH((k_norm_parts<A>), dim3((p.n + 31) / 32, 2), dim3(256), 0, st, (const A *)p.part, parts, p.n, wb, cb, wtype);
+        LA_LAUNCH((k_norm_parts<A>), dim3((p.n + 31) / 32, 2), dim3(1024), 0, st, (const A *)p.part, parts, p.n, wb, cb, wtype);
     return launch_check("layer norm");
 }
 
