@@ -219,7 +219,7 @@ __device__ __forceinline__ void stream_units(const char *src, uint32_t at)
                      : "m0", "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(at), "v"(off), "s"(src)
+                     "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:0xc00" ::"s"(at), "v"(off), "s"(src)
                      : "m0", "memory");
 }
 #pragma clang diagnostic pop

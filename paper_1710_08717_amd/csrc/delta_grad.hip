@@ -254,20 +254,20 @@ __global__ __launch_bounds__(128 * NG) void k_delta_scan_back(DeltaArgs p)
     }
 }
 
-// One block a chunk and key head, a wavefront for each 16 columns of Q_bar and K_bar over all tokens of the chunk.  The products summed over dv take 32
-// columns of O_bar, Z_bar and U at a time, through LDS, while the next 32 are loaded: once for M and N, once for the products with the states (all at once do
-// not fit the registers, and what does not fit waits for memory at every access).  M and N are formed as operands in both directions, by
-// exchanging the factors: their tiles go to LDS in units, split once, not by every wavefront that reads them.
+// One block a chunk and key head, a wavefront for each 16 columns of Q_bar and K_bar over all tokens of the chunk.  The products summed over dv take 128
+// columns of O_bar, Z_bar and U through LDS at a time.  M and N go through LDS in 32 bits; their operands, and those turned, are made of that once, in the place of the
+// columns, not by every wavefront that reads them.
 template <typename T, int DKP>
 __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 {
     using G = Pack<T, DKP>;
     constexpr int C = G::C, NI = G::NI, RT = G::RT, CS = G::CS, FT = G::FT, NW = DKP / 16, NT = 64 * NW;
-    constexpr int LZ = NI * RT, LU = LZ + NX * RT, STAGE = LU + NX * RT;  // units of 32 columns
+    constexpr int LZ = NI * RT, LU = LZ + NX * RT, STAGE = LU + NX * RT, WIDE = 4;  // units of 32 columns, and how many of those there are at a time
     constexpr int JM = 0, JN = NX * FT, JMT = 2 * NX * FT, JNT = 3 * NX * FT;  // units of M, N and turned M, beta N
-    constexpr bool BOTH = 2 * RT > NW;  // a wavefront forms a row and column tile of M and of N, else of one of them
-    __shared__ __align__(16) char stage[2][STAGE * UNIT];
-    __shared__ __align__(16) char joint[4 * NX * FT * UNIT];
+    constexpr bool BOTH = 2 * RT > NW;  // a wavefront forms a row tile of M and of N, else of one of them
+    static_assert(4 * FT * NX <= WIDE * STAGE, "M and N take the columns' place");
+    __shared__ __align__(16) char stage[WIDE * STAGE * UNIT];
+    __shared__ __align__(16) float mn[2][C][C + 4];
     __shared__ Decays<C> d;
     __shared__ __align__(16) float dots[4][NW][C];  // by wavefront: q.Q_bar, k.K_bar, k.H; last: k.(exp(b_last - b) U S1_bar^T)
     __shared__ float zv_box[C];
@@ -312,196 +312,170 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
     const bool form_m = BOTH || wave < RT, form_n = BOTH || (wave >= RT && wave < 2 * RT);
     const int tile = wave % RT;
 
+    // 8 columns of a row: of Z_bar and V, or of O_bar and U
+    constexpr int ROUNDS = (8 * C + NT - 1) / NT;
+    using Pack8 = PackOf<T, 8>;
+    struct Row {
+        f32x8 computed;              // Z_bar or U
+        typename Pack8::whole given;  // V or O_bar
+    };
+    const int steps = p.dvp / 32;
+    auto fetch = [&](Row *in, int h, int s) {
+        const int64_t sh = slot * p.hv + h;
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) {
+            in[k] = Row{};  // (or what was there before would be kept for the lanes that load nothing)
+            const int u = threadIdx.x + k * NT, r = u / 4 % C, c = 32 * s + 8 * (u % 4);
+            if (u < 8 * C) {
+                const bool z = u < 4 * C;
+                in[k].computed = load8<float>((z ? p.chunk_z_bar : p.chunk_u) + (sh * C + r) * (int64_t)p.dvp + c, 8);
+                const T *src = z ? (const T *)p.v + (t0 + r) * p.ldv + (int64_t)h * p.dv : (const T *)p.o_bar + ((t0 + r) * p.hv + h) * p.dv;
+                in[k].given = load_raw<T, 8>(src + c, r < len ? p.dv - c : 0);
+            }
+        }
+    };
     for (int h = hk * group; h < (hk + 1) * group; ++h) {
         const int64_t sh = slot * p.hv + h;
-        const float *S0 = p.chunk_state + sh * DKP * (int64_t)p.dvp + 8 * x4;
-        const float *S1 = p.chunk_state_bar + sh * DKP * (int64_t)p.dvp + 8 * x4;
-        const float *Ug = p.chunk_u + sh * C * (int64_t)p.dvp, *Zg = p.chunk_z_bar + sh * C * (int64_t)p.dvp;
+        const float *S0 = p.chunk_state + (sh * DKP + kcol) * (int64_t)p.dvp + 8 * x4;
+        const float *S1 = p.chunk_state_bar + (sh * DKP + kcol) * (int64_t)p.dvp + 8 * x4;
         if (wave == 0) {
             const char *pv = p.pack_v + sh * (int64_t)(G::value_units(true) * UNIT);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 *reinterpret_cast<f32x4 *>((char *)&d + i * UNIT + 16 * lane) = *reinterpret_cast<const f32x4 *>(pv + i * UNIT + 16 * lane);
         }
-        // row tile `tile` as columns of the accumulators (its rows the keys: M and N), column tile `tile` (its rows the queries: turned)
-        struct Pair {
-            f32x4 row[RT], turned[RT];
-        };
-        Pair pair[BOTH ? 2 : 1];  // of M, and of N in the last
+        f32x4 pair[BOTH ? 2 : 1][RT];  // M, and N in the last: columns the queries of tile `tile`, rows the keys
+        f32x4 a1[RT], a2[RT], a3[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            for (Pair &x : pair)
-                x.row[i] = x.turned[i] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < RT; ++i) {
+            a1[i] = a2[i] = a3[i] = f32x4{0, 0, 0, 0};
+            for (auto &x : pair)
+                x[i] = f32x4{0, 0, 0, 0};
+        }
         float zv = 0, states = 0;
-        // 8 columns of a row: of Z_bar and V, or of O_bar and U
-        constexpr int ROUNDS = (8 * C + NT - 1) / NT;
-        f32x8 in0[ROUNDS], in1[ROUNDS];
-        auto fetch = [&](int s, bool with_v) {
-#pragma unroll
-            for (int k = 0; k < ROUNDS; ++k) {
-                const int u = threadIdx.x + k * NT;
-                const int r = u / 4 % C, c = 32 * s + 8 * (u % 4);
-                if (u < 4 * C) {
-                    in0[k] = load8<float>(Zg + r * p.dvp + c, 8);
-                    if (with_v)
-                        in1[k] = load8<T>((const T *)p.v + (t0 + r) * p.ldv + (int64_t)h * p.dv + c, r < len ? p.dv - c : 0);
-                } else if (u < 8 * C) {
-                    in0[k] = load8<T>((const T *)p.o_bar + ((t0 + r) * p.hv + h) * p.dv + c, r < len ? p.dv - c : 0);
-                    in1[k] = load8<float>(Ug + r * p.dvp + c, 8);
-                }
-            }
+        f32x8 st0, st1;
+        auto fetch_states = [&](int s) {
+            st0 = load8<float>(S0 + 32 * s, 8);
+            st1 = load8<float>(S1 + 32 * s, 8);
         };
-        auto put = [&](char *at, bool with_v) {
+        for (int base = 0; base < steps; base += WIDE) {
+            if (base)
+                __syncthreads();  // the columns before are read
+            // one step's columns are loaded while the one before is put into LDS
+            const int until = steps < base + WIDE ? steps : base + WIDE;
+            auto put = [&](const Row *in, int s) {
 #pragma unroll
-            for (int k = 0; k < ROUNDS; ++k) {
-                const int u = threadIdx.x + k * NT;
-                const int r = u / 4 % C;
-                // token r: row 4 (r / 8 % 4) + r % 4 of tile 2 (r / 32) + r / 4 % 2
-                const int t = 2 * (r >> 5) + ((r >> 2) & 1);
-                char *to = at + 16 * (16 * (u % 4) + 4 * ((r >> 3) & 3) + (r & 3));
-                if (u < 4 * C) {
-                    if (with_v) {
+                for (int k = 0; k < ROUNDS; ++k) {
+                    const int u = threadIdx.x + k * NT, r = u / 4 % C;
+                    // token r: row 4 (r / 8 % 4) + r % 4 of tile 2 (r / 32) + r / 4 % 2
+                    const int t = 2 * (r >> 5) + ((r >> 2) & 1);
+                    char *to = stage + (s - base) * STAGE * UNIT + 16 * (16 * (u % 4) + 4 * ((r >> 3) & 3) + (r & 3));
+                    if (u < 8 * C) {
+                        const bool z = u < 4 * C;
+                        const Frag<NX> f = split<NX>(in[k].computed);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            zv += in0[k][i] * in1[k][i];
+                        for (int i = 0; i < NX; ++i)
+                            *reinterpret_cast<bf16x8 *>(to + ((z ? LZ : LU) + i * RT + t) * UNIT) = f.p[i];
+                        const f32x8 x = __builtin_convertvector(in[k].given, f32x8);
+                        if (z) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                zv += in[k].computed[i] * x[i];
+                        } else {
+                            const Frag<NI> o = split<NI>(x);
+#pragma unroll
+                            for (int i = 0; i < NI; ++i)
+                                *reinterpret_cast<bf16x8 *>(to + (i * RT + t) * UNIT) = o.p[i];
+                        }
                     }
-                    const Frag<NX> f = split<NX>(in0[k]);
-#pragma unroll
-                    for (int i = 0; i < NX; ++i)
-                        *reinterpret_cast<bf16x8 *>(to + (LZ + i * RT + t) * UNIT) = f.p[i];
-                } else if (u < 8 * C) {
-                    const Frag<NI> f = split<NI>(in0[k]);
-#pragma unroll
-                    for (int i = 0; i < NI; ++i)
-                        *reinterpret_cast<bf16x8 *>(to + (i * RT + t) * UNIT) = f.p[i];
-                    const Frag<NX> g = split<NX>(in1[k]);
-#pragma unroll
-                    for (int i = 0; i < NX; ++i)
-                        *reinterpret_cast<bf16x8 *>(to + (LU + i * RT + t) * UNIT) = g.p[i];
+                }
+            };
+            Row even[ROUNDS], odd[ROUNDS];
+            fetch(even, h, base);
+#pragma unroll 1
+            for (int s = base; s < until; s += 2) {
+                fetch(odd, h, s + 1 < until ? s + 1 : s);
+                put(even, s);
+                if (s + 1 < until) {
+                    fetch(even, h, s + 2 < until ? s + 2 : s);
+                    put(odd, s + 1);
                 }
             }
-        };
-        const int steps = p.dvp / 32;
-        int turn = 0;
-        fetch(0, true);
-        for (int s = 0; s < steps; ++s, turn ^= 1) {
-            char *at = stage[turn];
-            put(at, true);
             __syncthreads();
-            if (s + 1 < steps)
-                fetch(s + 1, true);
-            // M, N: whether this wavefront forms them; HIGH: its tile is in the second half of the tokens
+            if (base == 0)
+                fetch_states(0);
+            // M, N: whether this wavefront forms them; HIGH: its queries are in the second half of the tokens
             auto products = [&](auto M, auto N, auto HIGH) {
-                Frag<NI> ot;
-                Frag<NX> zt;
-                const Frag<NX> ut = unit<NX>(at, LU + tile, RT);
-                if constexpr (M.value)
-                    ot = unit<NI>(at, tile, RT);
-                if constexpr (N.value)
-                    zt = unit<NX>(at, LZ + tile, RT);
+#pragma unroll 1
+                for (int s = base; s < until; ++s) {
+                    const char *at = stage + (s - base) * STAGE * UNIT;
+                    Frag<NI> ot;
+                    Frag<NX> zt;
+                    if constexpr (M.value)
+                        ot = unit<NI>(at, tile, RT);
+                    if constexpr (N.value)
+                        zt = unit<NX>(at, LZ + tile, RT);
 #pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    const Frag<NX> u = unit<NX>(at, LU + i, RT);
-                    const bool row = CS == 1 || HIGH.value || i < 2, turned = CS == 1 || !HIGH.value || i >= 2;
-                    if constexpr (M.value) {
-                        if (row)
-                            mma<3>(pair[0].row[i], u, ot);
-                        if (turned)
-                            mma<3>(pair[0].turned[i], unit<NI>(at, i, RT), ut);
-                    }
-                    if constexpr (N.value) {
-                        if (row)
-                            mma<3>(pair[BOTH].row[i], u, zt);
-                        if (turned)
-                            mma<3>(pair[BOTH].turned[i], unit<NX>(at, LZ + i, RT), ut);
+                    for (int i = 0; i < (CS == 1 || HIGH.value ? RT : 2); ++i) {
+                        const Frag<NX> u = unit<NX>(at, LU + i, RT);
+                        if constexpr (M.value)
+                            mma<3>(pair[0][i], u, ot);
+                        if constexpr (N.value)
+                            mma<3>(pair[BOTH][i], u, zt);
                     }
                 }
             };
             using Yes = std::true_type;
             using No = std::false_type;
-            const bool high = CS > 1 && tile >= 2;
-            if constexpr (BOTH) {
-                if (high)
-                    products(Yes{}, Yes{}, Yes{});
+            auto halves = [&](auto M, auto N) {
+                if (CS > 1 && tile >= 2)
+                    products(M, N, Yes{});
                 else
-                    products(Yes{}, Yes{}, No{});
-            } else if (form_m) {
-                if (high)
-                    products(Yes{}, No{}, Yes{});
-                else
-                    products(Yes{}, No{}, No{});
-            } else if (form_n) {
-                if (high)
-                    products(No{}, Yes{}, Yes{});
-                else
-                    products(No{}, Yes{}, No{});
-            }
-        }
-        f32x8 st0, st1;
-        auto fetch_states = [&](int s) {
-            st0 = load8<float>(S0 + kcol * p.dvp + 32 * s, 8);
-            st1 = load8<float>(S1 + kcol * p.dvp + 32 * s, 8);
-        };
-        fetch(0, false);
-        fetch_states(0);
-        zv += __shfl_xor(zv, 1, 64);
-        zv += __shfl_xor(zv, 2, 64);
-        if (threadIdx.x < 4 * C && threadIdx.x % 4 == 0)
-            zv_box[threadIdx.x / 4] = zv;
-        // decays over M and N, and their units
-        const int mine = element_of(tile, col);  // this lane's token
-        f32x4 before[RT], after[RT];             // decays from token x to `mine`, from `mine` to x; zero where there is none
+                    products(M, N, No{});
+            };
+            if constexpr (BOTH)
+                halves(Yes{}, Yes{});
+            else if (form_m)
+                halves(Yes{}, No{});
+            else if (form_n)
+                halves(No{}, Yes{});
+            if (until == steps) {  // with the decays to LDS
+                const int mine = element_of(tile, col);  // this lane's query
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+                for (int i = 0; i < RT; ++i) {
+                    const int x = first_of(i);
+                    f32x4 e;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int x = first_of(i) + r;
-                before[i][r] = x <= mine ? d.between(mine, x) : 0.0f;
-                after[i][r] = mine <= x ? d.between(x, mine) : 0.0f;
-            }
-        auto put_joint = [&](Pair &y, bool m) {  // row: query `mine`, keys x; turned: queries x, key `mine`
+                    for (int r = 0; r < 4; ++r)
+                        e[r] = x + r <= mine ? d.between(mine, x + r) : 0.0f;
+                    if (form_m) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+                        for (int r = 0; r < 4; ++r)
+                            pair[0][i][r] = e[r] != 0 ? p.scale * e[r] * pair[0][i][r] : 0.0f;
+                        *reinterpret_cast<f32x4 *>(&mn[0][mine][x]) = pair[0][i];
+                    }
+                    if (form_n) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int x = first_of(i) + r;
-                    const float e = before[i][r], f = after[i][r];
-                    y.row[i][r] = m ? (e != 0 ? p.scale * e * y.row[i][r] : 0.0f) : (e != 0 && x != mine ? -e * y.row[i][r] : 0.0f);
-                    y.turned[i][r] = m ? (f != 0 ? p.scale * f * y.turned[i][r] : 0.0f) : (f != 0 && x != mine ? -d.walk.beta[x] * f * y.turned[i][r] : 0.0f);
+                        for (int r = 0; r < 4; ++r)
+                            pair[BOTH][i][r] = e[r] != 0 && x + r != mine ? -e[r] * pair[BOTH][i][r] : 0.0f;
+                        *reinterpret_cast<f32x4 *>(&mn[1][mine][x]) = pair[BOTH][i];
+                    }
                 }
-#pragma unroll
-            for (int s = 0; s < CS; ++s) {
-                if (s <= tile / 2)
-                    put_unit<NX>(joint, (m ? JM : JN) + G::lower(tile, s), FT, join(y.row[2 * s], y.row[2 * s + 1]));
-                if (s >= tile / 2)
-                    put_unit<NX>(joint, (m ? JMT : JNT) + G::upper(tile, s), FT, join(y.turned[2 * s], y.turned[2 * s + 1]));
             }
-        };
-        if (form_m)
-            put_joint(pair[0], true);
-        if (form_n)
-            put_joint(pair[BOTH], false);
-        f32x4 a1[RT], a2[RT], a3[RT];
+#pragma unroll 1
+            for (int s = base; s < until; ++s) {
+                const char *at = stage + (s - base) * STAGE * UNIT;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            a1[i] = a2[i] = a3[i] = f32x4{0, 0, 0, 0};
-        for (int s = 0; s < steps; ++s, turn ^= 1) {
-            char *at = stage[turn];
-            put(at, false);
+                for (int i = 0; i < 8; ++i)
+                    states += st0[i] * st1[i];
+                const Frag<NX> f0 = split<NX>(st0), f1 = split<NX>(st1);
+                fetch_states(s + 1 < steps ? s + 1 : s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                states += st0[i] * st1[i];
-            const Frag<NX> f0 = split<NX>(st0), f1 = split<NX>(st1);
-            __syncthreads();
-            if (s + 1 < steps) {
-                fetch(s + 1, false);
-                fetch_states(s + 1);
-            }
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                mma<3>(a2[i], unit<NX>(at, LZ + i, RT), f0);
-                mma<3>(a3[i], unit<NX>(at, LU + i, RT), f1);
-                mma<3>(a1[i], unit<NI>(at, i, RT), f0);
+                for (int i = 0; i < RT; ++i) {
+                    mma<3>(a2[i], unit<NX>(at, LZ + i, RT), f0);
+                    mma<3>(a3[i], unit<NX>(at, LU + i, RT), f1);
+                    mma<3>(a1[i], unit<NI>(at, i, RT), f0);
+                }
             }
         }
         Frag<NI> kt[CS], qt[CS];
@@ -510,6 +484,31 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
             kt[s] = unit<NI>(pk, G::KTURN + G::turned(wave, s), G::FK);
             qt[s] = unit<NI>(pk, G::QTURN + G::turned(wave, s), G::FK);
         }
+        __syncthreads();  // the columns are read: the operands take their place
+        char *joint = stage;
+        for (int u = wave; u < 4 * FT; u += NW) {  // M, N, turned M, turned beta N: FT units of each
+            const int which = u / FT, v = u % FT;
+            int i = v, s = 0;  // row tile and step of unit v
+            if constexpr (CS > 1) {
+                i = which < 2 ? (v < 2 ? v : 2 + (v - 2) / 2) : v < 4 ? v / 2 : v - 2;
+                s = which < 2 ? (v < 2 ? 0 : v & 1) : v < 4 ? v & 1 : 1;
+            }
+            const int row = element_of(i, col), at = 32 * s + 8 * x4;
+            f32x8 x;
+            if (which < 2) {
+                const float *from = &mn[which][row][at];
+                x = join(*reinterpret_cast<const f32x4 *>(from), *reinterpret_cast<const f32x4 *>(from + 4));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    x[r] = (which == 3 ? d.walk.beta[at + r] : 1.0f) * mn[which - 2][at + r][row];
+            }
+            put_unit<NX>(joint, which * NX * FT + v, FT, x);
+        }
+        zv += __shfl_xor(zv, 1, 64);
+        zv += __shfl_xor(zv, 2, 64);
+        if (threadIdx.x < 4 * C && threadIdx.x % 4 == 0)
+            zv_box[threadIdx.x / 4] = zv;
         const double sum = wave_sum((double)states);
         if (lane == 0)
             state_box[wave] = sum;
@@ -532,6 +531,7 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
             a3[i] *= d.walk.four(d.walk.out, first_of(i));
         }
         dot(3, a3, kt);
+        __syncthreads();  // M and N are there
 #pragma unroll
         for (int s = 0; s < CS; ++s)
 #pragma unroll
