@@ -339,7 +339,8 @@ la_status la_kalman_filter(la_dtype dt, int64_t batch, int T, int dh, int dv, in
  *   S_t = a_t S_{t-1} + k_t u_t^T,   a_t = exp(g_t),   u_t = beta_t (v_t - a_t S_{t-1}^T k_t),
  *   o_t = scale S_t^T q_t.
  * dt is LA_F32, LA_BF16 or LA_F16 (LA_F64: LA_ERR_UNSUPPORTED), the type of q, k, v, o and their gradients;
- * g, beta, the states and their gradients are float.  1 <= dk <= 128, 1 <= dv <= 1024 (above: LA_ERR_UNSUPPORTED).
+ * g, beta, the states and their gradients are float.  1 <= dk <= 128, 1 <= dv <= 1024, hv dv and
+ * ldv at most 2^24 (above: LA_ERR_UNSUPPORTED).
  * Value head h reads key head h / (hv / hk); hk divides hv.
  *   q, k [tokens of all sequences, hk, dk], v [.., hv, dv]: ldq, ldk, ldv elements from a token to the
  *   next (views of a wider projection); g, beta [.., hv], o [.., hv, dv] dense.
