@@ -228,13 +228,17 @@ la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *siz
             return LA_ERR_INVALID_ARG;
         const size_t b = (size_t)sizes[i] * bytes_of(types[i]);
         if (b && (!grads[i] || !out[i] || (uintptr_t)grads[i] % bytes_of(types[i]) || (uintptr_t)out[i] % bytes_of(types[i]) ||
-                  (grads[i] != out[i] && overlaps(grads[i], b, out[i], b)) || overlaps(norm, bytes_of(norm_type), out[i], b)))
+                  (grads[i] != out[i] && overlaps(grads[i], b, out[i], b)) || overlaps(norm, bytes_of(norm_type), out[i], b) || overlaps(norm, bytes_of(norm_type), grads[i], b)))
             return LA_ERR_INVALID_ARG;
     }
     const size_t need = la_clip_gradients_workspace_bytes(count, sizes);
     if (!need)
         return LA_ERR_UNSUPPORTED;
     LA_TRY(check_workspace(workspace, workspace_bytes, need, "la_clip_gradients_workspace_bytes"));
+    for (int i = 0; i < count; ++i)
+        if (any_overlap({{grads[i], (size_t)sizes[i] * bytes_of(types[i])}, {out[i], (size_t)sizes[i] * bytes_of(types[i])}, {norm, bytes_of(norm_type)}},
+                        {{workspace, need}}))
+            return LA_ERR_INVALID_ARG;
     ClipArgs a;
     a.part = (double *)workspace;
     a.max_norm = max_norm;

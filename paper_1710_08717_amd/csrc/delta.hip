@@ -874,9 +874,9 @@ la_status la_delta_rule(la_dtype dt, int64_t batch, int64_t tokens, int hk, int 
         return LA_ERR_INVALID_ARG;
     const size_t qs = z.all ? ((size_t)(z.all - 1) * ldq + (size_t)hk * dk) * es : 0, ks = z.all ? ((size_t)(z.all - 1) * ldk + (size_t)hk * dk) * es : 0,
                  vs = z.all ? ((size_t)(z.all - 1) * ldv + (size_t)hv * dv) * es : 0, gs = (size_t)z.all * hv * 4;
-    if (overlaps(o, ob, q, qs) || overlaps(o, ob, k, ks) || overlaps(o, ob, v, vs) || overlaps(o, ob, g, gs) || overlaps(o, ob, beta, gs) ||
-        overlaps(o, ob, initial_state, sb) || overlaps(o, ob, state, sb) || (state != initial_state && overlaps(state, sb, initial_state, sb)) ||
-        overlaps(state, sb, q, qs) || overlaps(state, sb, k, ks) || overlaps(state, sb, v, vs) || overlaps(state, sb, g, gs) || overlaps(state, sb, beta, gs))
+    const size_t fs = offsets ? ((size_t)batch + 1) * 4 : 0;
+    if (any_overlap({{q, qs}, {k, ks}, {v, vs}, {g, gs}, {beta, gs}, {offsets, fs}}, {{o, ob}, {state, sb}}) || overlaps(o, ob, initial_state, sb) ||
+        (state != initial_state && overlaps(state, sb, initial_state, sb)))
         return LA_ERR_INVALID_ARG;
     DeltaArgs p{q, k, v, ldq, ldk, ldv, g, beta, initial_state, offsets, batch, tokens, hk, hv, dk, dv, (float)scale, o, state};
     p.slots = z.slots;
@@ -884,8 +884,7 @@ la_status la_delta_rule(la_dtype dt, int64_t batch, int64_t tokens, int hk, int 
     void *base = saved ? saved : workspace;
     const size_t need = saved ? z.saved() : z.packets(false), given = saved ? saved_bytes : workspace_bytes;
     LA_TRY(check_workspace(base, given, need, saved ? "la_delta_rule_saved_bytes" : "la_delta_rule_workspace_bytes"));
-    if (overlaps(base, need, q, qs) || overlaps(base, need, k, ks) || overlaps(base, need, v, vs) || overlaps(base, need, o, ob) ||
-        overlaps(base, need, state, sb) || overlaps(base, need, initial_state, sb) || overlaps(base, need, g, gs) || overlaps(base, need, beta, gs))
+    if (any_overlap({{q, qs}, {k, ks}, {v, vs}, {g, gs}, {beta, gs}, {offsets, fs}, {o, ob}, {state, sb}, {initial_state, sb}}, {{base, need}}))
         return LA_ERR_INVALID_ARG;
     place_packets(p, z, base, saved != nullptr);
     return launch_delta_rule(dt, p, saved != nullptr, (hipStream_t)stream);
@@ -911,30 +910,18 @@ la_status la_delta_rule_backward(la_dtype dt, int64_t batch, int64_t tokens, int
                  sb = (size_t)batch * hv * dk * dv * 4;
     const size_t qs = z.all ? ((size_t)(z.all - 1) * ldq + (size_t)hk * dk) * es : 0, ks = z.all ? ((size_t)(z.all - 1) * ldk + (size_t)hk * dk) * es : 0,
                  vs = z.all ? ((size_t)(z.all - 1) * ldv + (size_t)hv * dv) * es : 0;
-    const struct {
-        const void *p;
-        size_t n;
-    } in[] = {{q, qs}, {k, ks}, {v, vs}, {g, gb}, {beta, gb}, {o_bar, ob}, {initial_state, sb}, {state_bar, sb}, {saved, saved_bytes}},
-      out[] = {{q_bar, qb}, {k_bar, qb}, {v_bar, ob}, {g_bar, gb}, {beta_bar, gb}, {initial_state_bar, sb}};
-    for (int i = 0; i < 6; ++i) {
-        for (const auto &x : in)
-            if (overlaps(out[i].p, out[i].n, x.p, x.n))
-                return LA_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (overlaps(out[i].p, out[i].n, out[j].p, out[j].n))
-                return LA_ERR_INVALID_ARG;
-    }
+    const size_t fs = offsets ? ((size_t)batch + 1) * 4 : 0;
+    const std::initializer_list<Span> in = {{q, qs}, {k, ks}, {v, vs}, {g, gb}, {beta, gb}, {offsets, fs}, {o_bar, ob}, {initial_state, sb}, {state_bar, sb}, {saved, saved_bytes}},
+                                      out = {{q_bar, qb}, {k_bar, qb}, {v_bar, ob}, {g_bar, gb}, {beta_bar, gb}, {initial_state_bar, sb}};
+    if (any_overlap(in, out))
+        return LA_ERR_INVALID_ARG;
     if (saved) {
         LA_TRY(check_workspace(saved, saved_bytes, z.saved(), "la_delta_rule_saved_bytes"));
     }
     const size_t need = la_delta_rule_backward_workspace_bytes(dt, batch, tokens, hk, hv, dk, dv, offsets != nullptr, saved != nullptr);
     LA_TRY(check_workspace(workspace, workspace_bytes, need, "la_delta_rule_backward_workspace_bytes"));
-    for (const auto &x : in)
-        if (overlaps(workspace, need, x.p, x.n))
-            return LA_ERR_INVALID_ARG;
-    for (const auto &x : out)
-        if (overlaps(workspace, need, x.p, x.n))
-            return LA_ERR_INVALID_ARG;
+    if (any_overlap(in, {{workspace, need}}) || any_overlap(out, {{workspace, need}}))
+        return LA_ERR_INVALID_ARG;
     hipStream_t st = (hipStream_t)stream;
     DeltaArgs p{q, k, v, ldq, ldk, ldv, g, beta, initial_state, offsets, batch, tokens, hk, hv, dk, dv, (float)scale};
     p.slots = z.slots;
@@ -979,14 +966,7 @@ la_status la_delta_rule_step(la_dtype dt, int64_t batch, int hk, int hv, int dk,
     const size_t es = bytes_of(dt), ob = (size_t)batch * hv * dv * es, sb = (size_t)slots * hv * dk * dv * 4, gb = (size_t)batch * hv * 4;
     const size_t qs = ((size_t)(batch - 1) * ldq + (size_t)hk * dk) * es, ks = ((size_t)(batch - 1) * ldk + (size_t)hk * dk) * es,
                  vs = ((size_t)(batch - 1) * ldv + (size_t)hv * dv) * es;
-    const struct {
-        const void *p;
-        size_t n;
-    } in[] = {{q, qs}, {k, ks}, {v, vs}, {g, gb}, {beta, gb}, {slot, (size_t)batch * 4}};
-    for (const auto &x : in)
-        if (overlaps(o, ob, x.p, x.n) || overlaps(state, sb, x.p, x.n))
-            return LA_ERR_INVALID_ARG;
-    if (overlaps(o, ob, state, sb))
+    if (any_overlap({{q, qs}, {k, ks}, {v, vs}, {g, gb}, {beta, gb}, {slot, (size_t)batch * 4}}, {{o, ob}, {state, sb}}))
         return LA_ERR_INVALID_ARG;
     DeltaStepArgs p{q, k, v, ldq, ldk, ldv, g, beta, state, slot, slots, hk, hv, dk, dv, 0, (float)scale, o};
     hipStream_t st = (hipStream_t)stream;

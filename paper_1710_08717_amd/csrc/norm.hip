@@ -477,8 +477,11 @@ la_status la_layer_norm(la_dtype dt, la_dtype wdt, int64_t rows, int n, int64_t 
         return LA_ERR_UNSUPPORTED;
     if (!x || !y || !mean != !rstd)
         return LA_ERR_INVALID_ARG;
-    const size_t xs = ((size_t)(rows - 1) * ldx + n) * bytes_of(dt), ys = (size_t)rows * n * bytes_of(dt), ws = (size_t)n * bytes_of(wdt);
-    if ((overlaps(x, xs, y, ys) && !(x == y && ldx == n)) || overlaps(weight, ws, y, ys) || overlaps(bias, ws, y, ys))
+    const size_t xs = ((size_t)(rows - 1) * ldx + n) * bytes_of(dt), ys = (size_t)rows * n * bytes_of(dt), ws = (size_t)n * bytes_of(wdt),
+                 ss = (size_t)rows * (dt == LA_F64 ? 8 : 4);
+    if (overlaps(x, xs, y, ys) && !(x == y && ldx == n))
+        return LA_ERR_INVALID_ARG;
+    if (any_overlap({{weight, ws}, {bias, ws}}, {{y, ys}}) || any_overlap({{x, xs}, {weight, ws}, {bias, ws}, {y, ys}}, {{mean, ss}, {rstd, ss}}))
         return LA_ERR_INVALID_ARG;
     NormArgs p{x, ldx, weight, bias, wdt != dt, nullptr, y, mean, rstd, nullptr, rows, n, eps};
     return norm_any(dt, p, false, nullptr, nullptr, wdt, (hipStream_t)stream);
@@ -508,13 +511,15 @@ la_status la_layer_norm_backward(la_dtype dt, la_dtype wdt, int64_t rows, int n,
         return LA_ERR_UNSUPPORTED;
     if (!x || !y_bar || !mean || !rstd || !x_bar)
         return LA_ERR_INVALID_ARG;
-    const size_t xs = ((size_t)(rows - 1) * ldx + n) * bytes_of(dt), ys = (size_t)rows * n * bytes_of(dt), ws = (size_t)n * bytes_of(wdt);
-    const size_t need = norm_parts_bytes(dt, rows, n);
-    if (overlaps(x, xs, x_bar, ys) || (y_bar != x_bar && overlaps(y_bar, ys, x_bar, ys)) || overlaps(weight, ws, x_bar, ys) ||
-        overlaps(weight_bar, ws, x_bar, ys) || overlaps(bias_bar, ws, x_bar, ys) || overlaps(weight_bar, ws, bias_bar, ws))
+    const size_t xs = ((size_t)(rows - 1) * ldx + n) * bytes_of(dt), ys = (size_t)rows * n * bytes_of(dt), ws = (size_t)n * bytes_of(wdt),
+                 ss = (size_t)rows * (dt == LA_F64 ? 8 : 4), need = norm_parts_bytes(dt, rows, n);
+    if (y_bar != x_bar && overlaps(y_bar, ys, x_bar, ys))
+        return LA_ERR_INVALID_ARG;
+    if (any_overlap({{x, xs}, {mean, ss}, {rstd, ss}, {weight, ws}}, {{x_bar, ys}, {weight_bar, ws}, {bias_bar, ws}}) ||
+        any_overlap({{y_bar, ys}, {x_bar, ys}}, {{weight_bar, ws}, {bias_bar, ws}}))
         return LA_ERR_INVALID_ARG;
     LA_TRY(check_workspace(workspace, workspace_bytes, need, "la_layer_norm_backward_workspace_bytes"));
-    if (overlaps(workspace, need, x, xs) || overlaps(workspace, need, y_bar, ys) || overlaps(workspace, need, x_bar, ys))
+    if (any_overlap({{x, xs}, {y_bar, ys}, {mean, ss}, {rstd, ss}, {weight, ws}, {x_bar, ys}, {weight_bar, ws}, {bias_bar, ws}}, {{workspace, need}}))
         return LA_ERR_INVALID_ARG;
     NormArgs p{x, ldx, weight, nullptr, wdt != dt, y_bar, x_bar, (void *)mean, (void *)rstd, workspace, rows, n, 0.0};
     return norm_any(dt, p, true, weight_bar, bias_bar, wdt, st);
