@@ -266,6 +266,7 @@ __global__ __launch_bounds__(128 * NG) void k_delta_scan(DeltaArgs p)
     __shared__ __align__(16) char turned[NI * FK * UNIT];
     __shared__ __align__(16) char vin[C * 16 * NG * sizeof(T)];
     __shared__ __align__(16) char ex1_all[NG][EX1], ex2_all[NG][EX2];
+    static_assert(!G::PAIRED || (NG == 2 && 2 * (sizeof(kq) + sizeof(tp) + sizeof(decays) + sizeof(turned) + sizeof(vin) + sizeof(ex1_all) + sizeof(ex2_all)) <= LDS_BYTES));
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, col = lane & 15;
     const int half = wave / NG, set = wave % NG;
     const unsigned block = block_of_die(p.slices);
@@ -612,9 +613,10 @@ static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
     if (p.slots > 0)
         LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
-    if (walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2)
+    using G = Pack<T, DKP>;
+    if (G::PAIRED || walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2)
         walk<T, DKP, 2, SAVE>(p, st);
-    else
+    else if constexpr (!G::PAIRED)
         walk<T, DKP, 4, SAVE>(p, st);
     return launch_check("delta rule");
 }

@@ -68,6 +68,7 @@ struct DeltaIn<float> {
 };
 
 constexpr int NX = 3;       // pieces of what is computed
+constexpr int LDS_BYTES = 160 * 1024;  // of a compute unit
 constexpr int UNIT = 1024;  // bytes of an operand of 16 rows, 32 summed elements and one piece, 16 a lane: "a unit"
 
 template <int N>
@@ -130,11 +131,6 @@ __device__ __forceinline__ unsigned block_of_die(unsigned slices)
     return b < whole ? (i / slices * 8 + b % 8) * slices + i % slices : b;
 }
 
-// Column groups of 16 of a walk's block: two where four would leave half of the compute units idle.  A block of two has a SIMD for every wavefront, and a chunk takes
-// it less time; with more blocks than compute units four groups share what they load (2 x 4096 tokens, 32 heads of 128, bf16:
-// the scans of the two passes take 311 and 314 us with two, 365 and 373 with four).
-inline int walk_groups(int64_t heads, int dv) { return heads * ((dv + 63) / 64) * 2 <= 256 ? 2 : 4; }
-
 // Two wavefronts share 16 columns of a walk: wavefront `half` keeps the state's rows and forms the chunk's tokens of its half of the tiles.  What the other one
 // needs of it passes through LDS: operands of a step (32 tokens), whose tiles a wavefront has both (RT = 4, step `half`) or one of (RT = 2).
 template <int RT>
@@ -167,6 +163,10 @@ struct Pack {
     static constexpr int RT = C / 16, KS = DKP / 32, KT = DKP / 16, CS = C / 32;
     static constexpr int NO = NI == 3 ? 3 : 2;  // pieces of what only the answers take: they are rounded to the input's type
     static constexpr int FK = RT * KS, FT = CS == 1 ? 2 : 6;
+    // Two blocks of two column groups of the forward walk fit the LDS side by side: always two then, the blocks of sequences of different lengths end more evenly
+    // (12 sequences of 1 to 2000 tokens, 12 heads, the whole call: f16 of 72 x 100 295 us with two, 309 with four, f32 of 64 216 and 256; of one length 0.98 to 1.04
+    // times as fast; where two do not fit, bf16 of 128, 252 and 222 us; the backward walk of one length is 1 to 5 % slower with two).
+    static constexpr bool PAIRED = C == 32 && NI * DKP <= 256;
     static constexpr int K = 0, Q = NI * FK, KTURN = 2 * NI * FK, QTURN = 3 * NI * FK;
     static constexpr int D = 0, TINV = 2, P = TINV + NX * FT, TTURN = P + NO * FT, PTURN = TTURN + NX * FT;
     static constexpr int key_units(bool save) { return (save ? 4 : 3) * NI * FK; }
@@ -177,6 +177,11 @@ struct Pack {
     static constexpr __host__ __device__ int lower(int i, int s) { return CS == 1 || i < 2 ? i : 2 * i - 2 + s; }
     static constexpr __host__ __device__ int upper(int i, int s) { return CS == 1 ? i : i < 2 ? 2 * i + s : 2 + i; }
 };
+
+// Column groups of 16 of a walk's block, two or four.  A block of two has a SIMD for every wavefront, and a chunk takes it less time: two where four would leave
+// half of the compute units idle (2 x 4096 tokens, 32 heads of 128, bf16: the scans of the two passes take 311 and 314 us with two, 365 and 373 with four).
+// With more blocks than compute units four share what they load.
+inline int walk_groups(int64_t heads, int dv) { return heads * ((dv + 63) / 64) * 2 <= 256 ? 2 : 4; }
 
 // a unit's operand: N pieces, `apart` units from one to the next
 template <int N>
