@@ -20,7 +20,9 @@ namespace la {
 // ---------------------------------------------------------------------------------
 // One block a chunk and key head.  K Q and K K^T are formed once and stay in accumulators, the decays of every value head are laid over them.  T is
 // formed by blocks: the 16 x 16 blocks of the diagonal by substitution, a column a lane, then twice the lower left block of a 2 x 2 block matrix,
-// -T22 (A21 T11), on the 32-bit matrix instruction.
+// -T22 (A21 T11), on the 32-bit matrix instruction.  Bound by the packets that it writes and by its steps' latency: 2 x 4096 tokens, 16 key and 32 value heads of
+// 128, bf16, everything kept: 127 us.  One block a chunk and value head where there are at most two such blocks a compute unit, which form K K^T and Q K^T
+// again: 3 x 333 tokens, 2 key and 6 value heads of 48 x 65, f32: 15 us instead of 22.
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 {
@@ -36,14 +38,15 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
     __shared__ __align__(16) Tiles m;
     __shared__ Decays<C> d;
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, col = lane & 15, x4 = lane >> 4;
-    const int hk = blockIdx.x % p.hk, group = p.hv / p.hk;
-    const int64_t slot = blockIdx.x / p.hk;
+    const int h0 = (int)(blockIdx.x % (p.hv / p.pack_heads)) * p.pack_heads, hk = h0 / (p.hv / p.hk);  // the first value head of this block, their key head
+    const bool first = h0 % (p.hv / p.hk) == 0;
+    const int64_t slot = blockIdx.x / (p.hv / p.pack_heads);
     if (p.offsets) {  // tokens of no sequence: zeros
         const int64_t a = p.offsets[0], z = p.offsets[p.batch];
         for (int64_t t = slot * C; t < (slot + 1) * C && t < p.tokens; ++t)
             if (t < a || t >= z)
-                for (int c = threadIdx.x; c < group * p.dv; c += 256)
-                    ((T *)p.o)[(t * p.hv + hk * group) * p.dv + c] = (T)0.0f;
+                for (int c = threadIdx.x; c < p.pack_heads * p.dv; c += 256)
+                    ((T *)p.o)[(t * p.hv + h0) * p.dv + c] = (T)0.0f;
     }
     int64_t t0;
     int len;
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
     }
     __syncthreads();
     char *pk = p.pack_k + (slot * p.hk + hk) * (int64_t)G::key_units(SAVE) * UNIT;
-    for (int u = wave; u < G::key_units(SAVE); u += 4)
+    for (int u = first ? wave : G::key_units(SAVE); u < G::key_units(SAVE); u += 4)
         *reinterpret_cast<bf16x8 *>(pk + u * UNIT + 16 * lane) = *reinterpret_cast<const bf16x8 *>(m.units + u * UNIT + 16 * lane);
     // row tile `wave` (of C = 32: tiles 0 and 1 by half of the wavefronts each half of the steps) of K K^T and Q K^T
     constexpr int NT = C == 64 ? RT : 1;  // column tiles of a wavefront
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
         }
     }
     const int i0 = first_of(ti);
-    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+    for (int h = h0; h < h0 + p.pack_heads; ++h) {
         __syncthreads();  // the units (or the head before) are read
         if (wave == 0)
             d.load(p.g + t0 * p.hv + h, p.beta + t0 * p.hv + h, p.hv, len);
@@ -244,10 +247,12 @@ __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 // A block takes NG groups of 16 columns of V, two wavefronts each.  A wavefront sums K S and Q S over its half of the state's rows, for all tokens, takes
 // the other half's sums for its half of the tokens, forms Z, U and the answers of those, and with everybody's U its half of the new state.  The packets of
 // the next chunk come straight to LDS, into the place of this one's as soon as all have read them.
+// Bound by the chain of chunks: 2 x 4096 tokens, 32 heads of 128, bf16, everything kept: 312 us, 64 chunks of 4.9 us with a block on every compute unit.  A wavefront's
+// 200 matrix instructions of a chunk are a quarter of that, the rest is splitting into pieces, the exchange and waiting with one wavefront a SIMD.
 //
 // Where sequences and heads are too few to fill the chip, a sequence is walked in segments side by side.  The state after a segment is M S + N with S the state
 // before it: MAP blocks find N (the walk from a state of zeros) and the columns of M (from the unit vectors, with V zero), without answers;
-// k_delta_join goes from segment to segment; then every segment is walked from its own state.
+// k_delta_join goes from segment to segment; then every segment is walked from its own state (8192 tokens, 16 heads of 128, bf16: 113, 22 and 80 us).
 template <typename T, int DKP, int NG, bool SAVE, bool MAP>
 __global__ __launch_bounds__(128 * NG) void k_delta_scan(DeltaArgs p)
 {
@@ -525,7 +530,7 @@ __global__ __launch_bounds__(128 * NG) void k_delta_scan(DeltaArgs p)
 }
 
 // From the state before a segment to the one after it, M S + N, over a sequence's segments: 16 columns of one head a block, 32 rows of the state a wavefront, its rows of
-// M loaded a segment ahead.
+// M loaded a segment ahead.  A chain of small products: 22 us over 8 segments of 16 heads of 128.
 template <int C, int DKP>
 __global__ __launch_bounds__(2 * DKP) void k_delta_join(DeltaArgs p)
 {
@@ -611,8 +616,9 @@ static void walk(DeltaArgs &p, hipStream_t st)
 template <typename T, int DKP, bool SAVE>
 static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
+    p.pack_heads = p.slots * p.hv <= 2 * COMPUTE_UNITS ? 1 : p.hv / p.hk;
     if (p.slots > 0)
-        LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * p.hk)), dim3(256), 0, st, p);
+        LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * (p.hv / p.pack_heads))), dim3(256), 0, st, p);
     using G = Pack<T, DKP>;
     if (G::PAIRED || walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2)
         walk<T, DKP, 2, SAVE>(p, st);
@@ -640,7 +646,8 @@ la_status launch_delta_rule(la_dtype dt, DeltaArgs p, bool save, hipStream_t st)
 // one token of every sequence
 // ---------------------------------------------------------------------------------
 // With s = S^T k and y = S^T q from one read of the state, the new state is a S + k u^T and the answer scale (a y + (q.k) u): the state is read and written
-// once, which is what bounds the call.  A block takes 32 columns of one state, its lanes packs of VEC columns by rows; all loads of a lane are in
+// once, which is what bounds the call (128 sequences, 32 heads of 128 x 128, bf16: 540 MB in 106 us, 5.1 TB/s, what a copy reaches; one sequence: 4.5 us, a
+// launch and one round trip).  A block takes 32 columns of one state, its lanes packs of VEC columns by rows; all loads of a lane are in
 // flight at once.
 struct DeltaStepArgs {
     const void *q, *k, *v;
@@ -747,7 +754,6 @@ static la_status step_t(DeltaStepArgs &p, int64_t batch, hipStream_t st)
 // sizes and buffers
 // ---------------------------------------------------------------------------------
 constexpr int DELTA_MAX_DK = 128, DELTA_MAX_DV = 1024;
-constexpr int64_t COMPUTE_UNITS = 256;
 constexpr int64_t DELTA_MAX_ROW = 1 << 24;  // elements of one token's row of v
 
 struct DeltaSizes {

@@ -45,6 +45,7 @@ struct DeltaArgs {
     void *q_bar, *k_bar, *v_bar;
     float *g_bar, *beta_bar, *state0_bar;
     int slices;  // blocks over dv
+    int pack_heads;  // value heads of a block of k_delta_pack
     // Few sequences and heads: they are walked in segments of `seg` chunks (0: whole).  By segment slot and value head: the state before it [DKP][dvp], and
     // the matrix [DKP][DKP] by which a segment's last state depends on its first.
     int seg;
@@ -68,6 +69,7 @@ struct DeltaIn<float> {
 };
 
 constexpr int NX = 3;       // pieces of what is computed
+constexpr int64_t COMPUTE_UNITS = 256;
 constexpr int LDS_BYTES = 160 * 1024;  // of a compute unit
 constexpr int UNIT = 1024;  // bytes of an operand of 16 rows, 32 summed elements and one piece, 16 a lane: "a unit"
 
