@@ -342,13 +342,22 @@ __global__ __launch_bounds__(128 * NG) void k_delta_scan(DeltaArgs p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = first_of(half * HK + t) + r;
-            if (part == 0)
+            if (part == 0 && (MAP || last))
                 S[t][r] = p.state0 && live && i < p.dk ? in_memory(p.state0)[state_at + (int64_t)i * p.dv + c0] : 0.0f;
             else if (MAP)
                 S[t][r] = unit_columns && i == c0 ? 1.0f : 0.0f;
             else
                 S[t][r] = kept ? in_memory(p.seg_state)[((sg * p.hv + h) * DKP + i) * p.dvp + c0] : 0.0f;
         }
+    // What the first of several segments is walked from later: by then the last one may have written its state over the initial one's, in place.
+    if (MAP && part == 0 && kept) {
+        float *to = p.seg_state + (sg * p.hv + h) * DKP * (int64_t)p.dvp;
+#pragma unroll
+        for (int t = 0; t < HK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                in_memory(to)[(int64_t)(first_of(half * HK + t) + r) * p.dvp + c0] = S[t][r];
+    }
     if (chunks > 0) {
         if (!half) {
             fetch_kq(pk);

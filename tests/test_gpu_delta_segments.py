@@ -42,3 +42,20 @@ def test_packed_sequences_of_few_heads(la, dtype, ends):  # noqa: F811
     ws = torch.full((96 << 20,), 255, dtype=torch.uint8, device="cuda")
     o3, _, _ = la.delta_rule(*[c[n] for n in t.ARGS], initial_state=state, offsets=at, workspace=ws)
     assert torch.equal(o, o3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_final_states_in_place_of_the_initial_ones(la, dtype):  # noqa: F811
+    """the first segment is walked from the state that it had, whenever the last one writes"""
+    w = t.make(dtype, 3, 2100, 1, 1, 48, 80, seed=8, decay=0.02)
+    c = t.cuda(w)
+    o, S, _ = la.delta_rule(*[c[n] for n in t.ARGS], initial_state=c["S0"], want_state=True)
+    lib, state, again = la.load(), c["S0"].clone(), torch.empty_like(o)
+    code = 2 if dtype == BF16 else 0
+    size = (code, 3, 2100, 1, 1, 48, 80)
+    ws = torch.empty(int(lib.la_delta_rule_workspace_bytes(*size, 0)), dtype=torch.uint8, device="cuda")
+    q, k, v, g, beta = (c[n] for n in t.ARGS)
+    rc = lib.la_delta_rule(*size, None, q.data_ptr(), 48, k.data_ptr(), 48, v.data_ptr(), 80, g.data_ptr(), beta.data_ptr(), 48 ** -0.5, state.data_ptr(),
+                           again.data_ptr(), state.data_ptr(), None, 0, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    assert torch.equal(o, again) and torch.equal(S, state)
