@@ -47,6 +47,11 @@ class DeltaRule(torch.autograd.Function):
         return la.delta_rule_backward(*inputs, o_bar.contiguous(), saved=kept)[:5]
 
 
+def product(x, weight):
+    """x weight^T as one matrix product over all tokens"""
+    return (x.flatten(0, -2) @ weight.to(x.dtype).T).unflatten(0, x.shape[:-1])
+
+
 class Block(torch.nn.Module):
     def __init__(self, width, key_heads, value_heads, head):
         super().__init__()
@@ -60,28 +65,28 @@ class Block(torch.nn.Module):
     def inputs(self, y):
         """q, k, v, g, beta of the normalised tokens; the last axis of y is the width"""
         lead = y.shape[:-1]
-        q, k, v, a, b = (y @ self.project.to(y.dtype).T).split(self.sizes, dim=-1)
+        q, k, v, a, b = product(y, self.project).split(self.sizes, dim=-1)
         q, k = (F.normalize(x.reshape(*lead, self.key_heads, self.head).float(), dim=-1).to(y.dtype) for x in (q, k))
         v = v.unflatten(-1, (self.value_heads, self.head))  # a view: its tokens lie a row of the product apart
         return q, k, v, -F.softplus(a.float() + self.decay), torch.sigmoid(b.float())
 
     def forward(self, x):
         o = DeltaRule.apply(*self.inputs(LayerNorm.apply(x, self.weight, self.bias)))
-        return x + o.flatten(-2) @ self.out.to(x.dtype).T
+        return x + product(o.flatten(-2), self.out)
 
     @torch.no_grad()
     def prompt(self, x):
         """the block of a whole prompt, and the state after it"""
         q, k, v, g, beta = self.inputs(la.layer_norm(x, self.weight, self.bias)[0])
         o, state, _ = la.delta_rule(q, k, v, g, beta, want_state=True)
-        return x + o.flatten(-2) @ self.out.to(x.dtype).T, state
+        return x + product(o.flatten(-2), self.out), state
 
     @torch.no_grad()
     def step(self, x, state):
         """one token of every sequence; the state is updated in place"""
         q, k, v, g, beta = self.inputs(la.layer_norm(x, self.weight, self.bias)[0])
         o = la.delta_rule_step(q, k, v, g, beta, state)
-        return x + o.flatten(-2) @ self.out.to(x.dtype).T
+        return x + product(o.flatten(-2), self.out)
 
 
 class Recall(torch.nn.Module):
@@ -97,7 +102,7 @@ class Recall(torch.nn.Module):
         return (self.keys[key] + self.values[value]).to(self.dtype)
 
     def logits(self, y):
-        return (y @ self.answer.to(y.dtype).T).float()
+        return product(y, self.answer).float()
 
     def forward(self, key, value):
         x = self.embed(key, value)

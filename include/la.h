@@ -384,7 +384,8 @@ la_status la_delta_rule_step(la_dtype dt, int64_t batch, int hk, int hv, int dk,
 
 /* Layer norm of rows of n elements: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps).  x: row r starts
  * at x + r ldx; y [rows, n] dense (it may be x where ldx == n).  weight, bias [n] of type wdt, or NULL (1 and 0): wdt is dt, or
- * LA_F32 where dt is 16 bits wide.  mean, rstd [rows], both or neither: float, double for LA_F64; the gradient takes them. */
+ * LA_F32 where dt is 16 bits wide.  mean, rstd [rows], both or neither: float, double for LA_F64; the gradient takes them
+ * (zeros where n = 0). */
 la_status la_layer_norm(la_dtype dt, la_dtype wdt, int64_t rows, int n, int64_t ldx, const void *x, const void *weight, const void *bias,
                         double eps, void *y, void *mean, void *rstd, void *stream);
 

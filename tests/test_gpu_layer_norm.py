@@ -149,3 +149,10 @@ def test_refusals(la):
                  lambda: la.layer_norm_backward(x, x, mean, rstd, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(la.LaError):
             call()
+
+
+def test_rows_of_nothing(la):
+    x = torch.empty(5, 0, device="cuda", dtype=torch.bfloat16)
+    y, mean, rstd = la.layer_norm(x, want_stats=True)
+    assert y.shape == x.shape and not mean.any() and not rstd.any()
+    assert all(t.numel() == 0 for t in la.layer_norm_backward(x, y, mean, rstd))
