@@ -22,7 +22,8 @@ namespace la {
 // formed by blocks: the 16 x 16 blocks of the diagonal by substitution, a column a lane, then twice the lower left block of a 2 x 2 block matrix,
 // -T22 (A21 T11), on the 32-bit matrix instruction.  Bound by the packets that it writes and by its steps' latency: 2 x 4096 tokens, 16 key and 32 value heads of
 // 128, bf16, everything kept: 127 us.  One block a chunk and value head where there are at most two such blocks a compute unit, which form K K^T and Q K^T
-// again: 3 x 333 tokens, 2 key and 6 value heads of 48 x 65, f32: 15 us instead of 22.
+// again: 3 x 333 tokens, 2 key and 6 value heads of 48 x 65, f32: 15 us instead of 22 (the whole call of 1024 tokens, 16 / 32 heads of 128, bf16, 512 such
+// blocks: 71 and 77; of 4096 tokens, 4 / 32 heads, 2048 of them: 240 and 237).
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(256) void k_delta_pack(DeltaArgs p)
 {
@@ -814,11 +815,11 @@ static la_status delta_sizes(la_dtype dt, int64_t batch, int64_t tokens, int hk,
     if (z.slots > most / hv || batch > most / hv / ((dv + 15) / 16))  // blocks of one launch
         return LA_ERR_UNSUPPORTED;
     const size_t heads = (size_t)z.slots * hv;
-    // Segments where whole sequences would leave more than two thirds of the compute units idle, as many as fill them, of 8 chunks at least and up to 8 of a
-    // sequence of the average length: a sequence of g segments takes the time of about 2 / g of it (16 heads of 128, 8192 tokens, bf16:
-    // 0.25 ms the whole call, 0.54 without segments).
+    // Segments where whole sequences would leave three quarters of the compute units idle, as many as fill them, of 8 chunks at least and up to 8 of a
+    // sequence of the average length: a sequence of g segments takes the time of about 2 / g of it (heads of 128, bf16, in us with and without: 8192 tokens,
+    // 16 heads 250 and 540, 32 heads 530 and 583, 40 heads, which make three segments, 685 and 620; 16 heads, 24 chunks 81 and 99, 16 chunks 71 and 66).
     const int64_t blocks = batch * hv * ((dv + 63) / 64);
-    if (blocks > 0 && blocks * 3 <= COMPUTE_UNITS) {
+    if (blocks > 0 && blocks * 4 <= COMPUTE_UNITS) {
         const int64_t each = (z.all / batch + z.c - 1) / z.c, most_parts = COMPUTE_UNITS / blocks < 8 ? COMPUTE_UNITS / blocks : 8;
         const int64_t seg = (each + most_parts - 1) / most_parts;
         if (each >= 24) {
