@@ -565,13 +565,14 @@ __global__ __launch_bounds__(2 * DKP) void k_delta_join(DeltaArgs p)
             for (int r = 0; r < 4; ++r)
                 x[i][r] = in_memory(at(g))[(int64_t)(first_of(2 * wave + i) + r) * p.dvp];
     };
+    // M's columns are there up to dk, by the 32: rows of the state past dk are zero, and what the workspace holds in their columns of M may be NaN.
     auto map_of = [&](int64_t g) {
         const float *M = p.seg_map + (g * p.hv + h) * DKP * (int64_t)DKP;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int s = 0; s < KS; ++s)
-                m[i][s] = load8<float>(M + element_of(2 * wave + i, col) * DKP + 32 * s + 8 * x4, 8);
+                m[i][s] = 32 * s < p.dk ? load8<float>(M + element_of(2 * wave + i, col) * DKP + 32 * s + 8 * x4, 8) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
     };
     rows_of(sg + 1, S);
     map_of(sg + 1);
