@@ -769,8 +769,8 @@ def layer_norm_backward(x, y_bar, mean, rstd, weight=None, want_weights=True, ou
 
 def clip_gradients(grads, max_norm, out=None, workspace=None):
     """la_clip_gradients: scales all tensors of ``grads`` by min(1, max_norm / norm) over all of them, into ``out`` (as many tensors of the same
-    shapes and dtypes) or in place.  Returns the norm before it, on the GPU (float64 where a gradient is, else float32); where it is not finite the
-    gradients are passed on unchanged."""
+    shapes and dtypes) or in place; no output overlaps another gradient or output, so that a tensor is not there twice in place.  Returns the norm before it, on the
+    GPU (float64 where a gradient is, else float32); where it is not finite the gradients are passed on unchanged."""
     if _host is not None and workspace is None:
         r = _host.clip_gradients(grads, max_norm, out)
         if r is not None:
