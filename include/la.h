@@ -398,9 +398,10 @@ la_status la_layer_norm_backward(la_dtype dt, la_dtype wdt, int64_t rows, int n,
 
 /* The norm over all of `count` gradients, norm = sqrt(sum of their squares), and out = gradient * min(1, max_norm / norm).  types,
  * sizes (elements), grads, out: HOST arrays, their pointers device memory; out[i] is grads[i] (in place) or does not overlap any
- * gradient, and no output overlaps another or another's gradient (LA_ERR_INVALID_ARG: a tensor cannot be there twice in place).  norm: one element of norm_type (LA_F32 or LA_F64), on the device.  Where the norm is not finite the gradients are
- * passed on unchanged: the caller sees it in norm.  Squares are summed in 64 bits, in an order that depends on sizes and
- * addresses' alignment alone.  max_norm >= 0, infinity as well (the norm alone). */
+ * gradient, and no output overlaps another or another's gradient (LA_ERR_INVALID_ARG: a tensor cannot be there twice in place).
+ * norm: one element of norm_type (LA_F32 or LA_F64), on the device.  Where the norm is not finite, or past the largest number of
+ * norm_type, the gradients are passed on unchanged: the caller sees it in norm.  Squares are summed in 64 bits, in an order that
+ * depends on sizes and addresses' alignment alone.  max_norm >= 0, infinity as well (the norm alone). */
 size_t la_clip_gradients_workspace_bytes(int count, const int64_t *sizes);
 la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *sizes, const void *const *grads, void *const *out,
                             double max_norm, la_dtype norm_type, void *norm, void *workspace, size_t workspace_bytes, void *stream);

@@ -1,6 +1,6 @@
 // The norm over all gradients of a model, and the gradients scaled to a largest norm.
 //
-//   norm = sqrt(sum over all tensors of x^2),   out = x min(1, max_norm / norm);  factor 1 where the norm is not finite (or zero)
+//   norm = sqrt(sum over all tensors of x^2),   out = x min(1, max_norm / norm);  factor 1 where the norm, as it is written out, is not finite (or zero)
 //
 // Two passes over the data, since the factor is known after the first only: bound by memory.  Squares are summed in 64 bits, which no gradient
 // overflows (the squares of float's largest values do in 32), and in an order that depends on the sizes alone.  A launch takes the pointers of up to
@@ -151,7 +151,8 @@ __global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs a)
     for (int i = threadIdx.x; i < a.parts; i += 256)
         s += a.part[i];
     const double norm = sqrt(block_sum(s));
-    const double factor = norm > a.max_norm && norm < INFINITY ? a.max_norm / norm : 1.0;
+    const double seen = a.norm64 ? norm : (double)(float)norm;  // (what the caller tells by that nothing was scaled)
+    const double factor = norm > a.max_norm && seen < INFINITY ? a.max_norm / norm : 1.0;
     if (a.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
         if (a.norm64)
             *(double *)a.norm = norm;
