@@ -2,8 +2,9 @@
 //
 //   norm = sqrt(sum over all tensors of x^2),   out = x min(1, max_norm / norm);  factor 1 where the norm, as it is written out, is not finite (or zero)
 //
-// Two passes over the data, since the factor is known after the first only: bound by memory.  Squares are summed in 64 bits, which no gradient
-// overflows (the squares of float's largest values do in 32), and in an order that depends on the sizes alone.  A launch takes the pointers of up to
+// Two passes over the data, since the factor is known after the first only: bound by memory.  Squares are summed in 64 bits, which those of float's largest and
+// smallest numbers fit (not so in 32); doubles whose squares do not are scaled into sums of their own.  The order of the sums depends on sizes and addresses'
+// alignment alone.  A launch takes the pointers of up to
 // CLIP_TENSORS tensors among its arguments, so that no table is copied to the device.  290 tensors of 200 million elements, matrices in bf16: the squares of 400 MB
 // in 108 us (3.7 TB/s: the conversions to 64 bits stand beside the loads), the scaling of 800 MB in 148 us (5.4 TB/s), each in three launches; 24 tensors of
 // 20 thousand elements: 4.2 and 5.5 us.
@@ -29,7 +30,8 @@ struct ClipArgs {
     uint8_t type[CLIP_TENSORS];
     int count;
     int parts;       // partial sums of all launches
-    double *part;    // the whole array
+    double *part;    // the whole array; with `wide` two more behind it, of large and of small doubles
+    int wide;        // whether any tensor is of doubles
     int part0;       // where this launch's partial sums start
     double max_norm;
     void *norm;      // written by the first launch of the second pass
@@ -37,6 +39,8 @@ struct ClipArgs {
 };
 static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
 
+// (a box for each WHICH: sums one after another need no barrier in between)
+template <int WHICH>
 __device__ __forceinline__ double block_sum(double x)
 {
     __shared__ double box[4];
@@ -46,6 +50,32 @@ __device__ __forceinline__ double block_sum(double x)
     __syncthreads();
     return box[0] + box[1] + box[2] + box[3];
 }
+
+// A lane's sum of squares: in `mid` of numbers between 2^-480 and 2^480 and of zeros, so that neither one square nor the sum of 2^63 of them leaves the range; larger
+// and smaller ones, doubles only, by 2^-600 and 2^600.  A NaN is in one of them.
+struct Squares {
+    double mid = 0, large = 0, small = 0;
+    __device__ __forceinline__ void add(float x) { mid += (double)x * (double)x; }
+    __device__ __forceinline__ void add(double x)
+    {
+        const double size = fabs(x);
+        if (size > 0x1p480)
+            large += (x * 0x1p-600) * (x * 0x1p-600);
+        else if (size < 0x1p-480)
+            small += (x * 0x1p600) * (x * 0x1p600);
+        else
+            mid += x * x;
+    }
+    // the root of the sum of all
+    __device__ __forceinline__ double norm() const
+    {
+        if (large != 0)
+            return sqrt(large + mid * 0x1p-600 * 0x1p-600) * 0x1p600;
+        if (mid != 0)
+            return sqrt(mid + small * 0x1p-600 * 0x1p-600);
+        return sqrt(small) * 0x1p-600;
+    }
+};
 
 // The tensor of a tile: the last one whose first tile is not past it.
 __device__ __forceinline__ int tensor_of(const ClipArgs &a, uint32_t tile)
@@ -64,17 +94,14 @@ __device__ __forceinline__ int tensor_of(const ClipArgs &a, uint32_t tile)
 // One tile of a tensor, f(first, count elements at p) in packs of 16 bytes where they start on one, one element at a time before and after.
 // `lead`: elements before the first whole pack of the tensor.
 template <typename T>
-__device__ __forceinline__ double tile_squares(const T *p, int64_t n, uint32_t tile)
+__device__ __forceinline__ void tile_squares(Squares &s, const T *p, int64_t n, uint32_t tile)
 {
     constexpr int VEC = 16 / sizeof(T);
     const int64_t lead = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T);
     const int64_t from = tile ? lead + (int64_t)tile * CLIP_TILE : 0, to0 = lead + ((int64_t)tile + 1) * CLIP_TILE, to = to0 < n ? to0 : n;
-    double s = 0;
     int64_t at = tile ? from : (lead < n ? lead : n);
-    if (!tile && threadIdx.x < at) {
-        const double x = (double)(acc_of<T>)p[threadIdx.x];
-        s += x * x;
-    }
+    if (!tile && threadIdx.x < at)
+        s.add((acc_of<T>)p[threadIdx.x]);
     const int64_t packs = to > at ? (to - at) / VEC : 0;
 #pragma unroll 4
     for (int64_t i = threadIdx.x; i < packs; i += 256) {
@@ -82,32 +109,37 @@ __device__ __forceinline__ double tile_squares(const T *p, int64_t n, uint32_t t
         load_pack<T, VEC>(p + at + i * VEC, v);
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-            s += (double)v[j] * (double)v[j];
+            s.add(v[j]);
     }
     at += packs * VEC;
-    if (at + threadIdx.x < to) {
-        const double x = (double)(acc_of<T>)p[at + threadIdx.x];
-        s += x * x;
-    }
-    return s;
+    if (at + threadIdx.x < to)
+        s.add((acc_of<T>)p[at + threadIdx.x]);
 }
 
 __global__ __launch_bounds__(256) void k_grad_squares(const ClipArgs a)
 {
-    double s = 0;
+    Squares s;
     for (uint32_t t = blockIdx.x; t < a.first[a.count]; t += gridDim.x) {
         const int k = tensor_of(a, t);
         const uint32_t tile = t - a.first[k];
         switch (a.type[k]) {
-        case LA_F32: s += tile_squares((const float *)a.src[k], a.n[k], tile); break;
-        case LA_F64: s += tile_squares((const double *)a.src[k], a.n[k], tile); break;
-        case LA_BF16: s += tile_squares((const bf16_t *)a.src[k], a.n[k], tile); break;
-        default: s += tile_squares((const f16_t *)a.src[k], a.n[k], tile); break;
+        case LA_F32: tile_squares(s, (const float *)a.src[k], a.n[k], tile); break;
+        case LA_F64: tile_squares(s, (const double *)a.src[k], a.n[k], tile); break;
+        case LA_BF16: tile_squares(s, (const bf16_t *)a.src[k], a.n[k], tile); break;
+        default: tile_squares(s, (const f16_t *)a.src[k], a.n[k], tile); break;
         }
     }
-    s = block_sum(s);
+    const int at = a.part0 + blockIdx.x;
+    const double mid = block_sum<0>(s.mid);
     if (threadIdx.x == 0)
-        a.part[a.part0 + blockIdx.x] = s;
+        a.part[at] = mid;
+    if (a.wide) {
+        const double large = block_sum<1>(s.large), small = block_sum<2>(s.small);
+        if (threadIdx.x == 0) {
+            a.part[a.parts + at] = large;
+            a.part[2 * a.parts + at] = small;
+        }
+    }
 }
 
 template <typename T>
@@ -147,10 +179,19 @@ __device__ __forceinline__ void tile_scale(const T *p, T *q, int64_t n, uint32_t
 // Every block sums the partial sums itself, in the same order: no launch in between.
 __global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs a)
 {
-    double s = 0;
+    Squares s;
     for (int i = threadIdx.x; i < a.parts; i += 256)
-        s += a.part[i];
-    const double norm = sqrt(block_sum(s));
+        s.mid += a.part[i];
+    s.mid = block_sum<0>(s.mid);
+    if (a.wide) {
+        for (int i = threadIdx.x; i < a.parts; i += 256) {
+            s.large += a.part[a.parts + i];
+            s.small += a.part[2 * a.parts + i];
+        }
+        s.large = block_sum<1>(s.large);
+        s.small = block_sum<2>(s.small);
+    }
+    const double norm = s.norm();
     const double seen = a.norm64 ? norm : (double)(float)norm;  // (what the caller tells by that nothing was scaled)
     const double factor = norm > a.max_norm && seen < INFINITY ? a.max_norm / norm : 1.0;
     if (a.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
@@ -266,7 +307,7 @@ size_t la_clip_gradients_workspace_bytes(int count, const int64_t *sizes)
             return LA_OK;
         }) != LA_OK)
         return 0;
-    return align_up(parts * sizeof(double));
+    return align_up(3 * parts * sizeof(double));  // (the types are not known here)
 }
 
 la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *sizes, const void *const *grads, void *const *out, double max_norm,
@@ -301,6 +342,9 @@ la_status la_clip_gradients(int count, const la_dtype *types, const int64_t *siz
     a.max_norm = max_norm;
     a.norm = norm;
     a.norm64 = norm_type == LA_F64;
+    a.wide = 0;
+    for (int i = 0; i < count; ++i)
+        a.wide |= types[i] == LA_F64;
     a.parts = 0;
     LA_TRY(clip_launches(count, sizes, [&](int, int, int64_t tiles) {
         a.parts += clip_blocks(tiles);

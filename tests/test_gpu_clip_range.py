@@ -80,3 +80,54 @@ def test_the_largest_norm_that_32_bits_hold_is_clipped(la):
     want = x.double() * (2.0 / value(norm_of([x])))
     norm = la.clip_gradients([x], 2.0)
     assert math.isfinite(float(norm)) and f.rel(x, want) <= f.tolerance(F32)
+
+
+@pytest.mark.parametrize("sizes", [(1e200,), (1e-200,), (1e306, 1e300, 1.0), (1e200, 1.0, 1e-200), (1.0, 1e-200), (1e145, 1e146), (1e-146, 1e-144), (1e-308,), (4e-320,)])
+def test_squares_that_64_bits_do_not_hold(la, sizes):
+    grads = [make(9001 + 100 * i, s, F64, seed=i) for i, s in enumerate(sizes)]
+    norm = norm_of(grads)
+    for limit in (0.25 * value(norm), 4.0 * value(norm)):
+        out = [torch.empty_like(x) for x in grads]
+        got = la.clip_gradients(grads, limit, out=out)
+        # (numbers below 2^-1022 are rounded to a multiple of 2^-1074)
+        assert abs(float(got) - value(norm)) <= 1e-12 * value(norm) + 2.0 ** -1074
+        if limit > value(norm):
+            assert all(same(a, b) for a, b in zip(out, grads))
+        else:
+            for a, b in zip(out, grads):
+                assert bool(((a - 0.25 * b).abs() <= 1e-12 * b.abs() + 2.0 ** -1073).all())
+    assert value(norm_of(out)) > 0
+
+
+def test_many_large_squares(la):
+    """what is just below the limit between two sums does not overflow by its number"""
+    grads = [make(3_000_000, s, F64) for s in (2.0 ** 479, 2.0 ** -479, 2.0 ** 481)]
+    for x in grads:
+        assert abs(float(la.clip_gradients([x.clone()], math.inf)) / value(norm_of([x])) - 1) <= 1e-12
+
+
+def test_large_doubles_beside_other_types(la):
+    grads = [make(500, 1e250, F64), make(300, 3e38, F32), make(20, 1e-40, BF16), make(99, 60000.0, F16)]
+    norm = value(norm_of(grads))
+    want = [x.double() * (1e245 / norm) for x in grads]
+    out = [torch.empty_like(x) for x in grads]
+    assert abs(float(la.clip_gradients(grads, 1e245, out=out)) / norm - 1) <= 1e-12
+    for x, y in zip(out[:2] + out[3:], want[:2] + want[3:]):  # (the third is below the smallest number of its type)
+        assert f.rel(x, y) <= f.tolerance(x.dtype)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("rest", [1e300, 1.0, 1e-300, 0.0])
+def test_doubles_that_are_not_finite_change_nothing(la, bad, rest):
+    grads = [make(4000, rest, F64), make(5, rest, F64)]
+    grads[1][2] = bad
+    before = [x.clone() for x in grads]
+    norm = float(la.clip_gradients(grads, 1e-3))
+    assert math.isnan(norm) if math.isnan(bad) else norm == math.inf
+    assert all(same(a, b) for a, b in zip(grads, before))
+
+
+def test_a_double_norm_past_its_range_changes_nothing(la):
+    x = make(1000, 1.7e308, F64)
+    y = x.clone()
+    assert float(la.clip_gradients([x], 1.0)) == math.inf and same(x, y)
