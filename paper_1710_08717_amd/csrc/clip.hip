@@ -143,14 +143,23 @@ __global__ __launch_bounds__(256) void k_grad_squares(const ClipArgs a)
 }
 
 template <typename T>
-__device__ __forceinline__ void tile_scale(const T *p, T *q, int64_t n, uint32_t tile, double factor)
+__device__ __forceinline__ void tile_scale(const ClipArgs &a, const T *p, T *q, int64_t n, uint32_t tile, double factor, double norm)
 {
     using A = acc_of<T>;
     constexpr int VEC = 16 / sizeof(T);
     const A f = (A)factor;
+    // a factor below A's smallest normal number has few bits in A, and the largest elements times it may not be small: elements divided by 2^100 in 64 bits (which no
+    // product above the smallest number of T notices) times the factor times 2^100
+    const bool denormal = a.max_norm > 0 && factor < (sizeof(A) == 8 ? 0x1p-1022 : 0x1p-126);
     const int64_t lead = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T);
     const int64_t to0 = lead + ((int64_t)tile + 1) * CLIP_TILE, to = to0 < n ? to0 : n;
     int64_t at = tile ? lead + (int64_t)tile * CLIP_TILE : 0;
+    if (denormal) {
+        const double g = a.max_norm / (norm * 0x1p-100);
+        for (int64_t i = at + threadIdx.x; i < to; i += 256)
+            q[i] = (T)(A)((double)(A)p[i] * 0x1p-100 * g);
+        return;
+    }
     if (((uintptr_t)p & 15) != ((uintptr_t)q & 15)) {  // no pack starts on 16 bytes in both
         for (int64_t i = at + threadIdx.x; i < to; i += 256)
             q[i] = (T)((A)p[i] * f);
@@ -206,10 +215,10 @@ __global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs a)
             continue;
         const uint32_t tile = t - a.first[k];
         switch (a.type[k]) {
-        case LA_F32: tile_scale((const float *)a.src[k], (float *)a.dst[k], a.n[k], tile, factor); break;
-        case LA_F64: tile_scale((const double *)a.src[k], (double *)a.dst[k], a.n[k], tile, factor); break;
-        case LA_BF16: tile_scale((const bf16_t *)a.src[k], (bf16_t *)a.dst[k], a.n[k], tile, factor); break;
-        default: tile_scale((const f16_t *)a.src[k], (f16_t *)a.dst[k], a.n[k], tile, factor); break;
+        case LA_F32: tile_scale(a, (const float *)a.src[k], (float *)a.dst[k], a.n[k], tile, factor, norm); break;
+        case LA_F64: tile_scale(a, (const double *)a.src[k], (double *)a.dst[k], a.n[k], tile, factor, norm); break;
+        case LA_BF16: tile_scale(a, (const bf16_t *)a.src[k], (bf16_t *)a.dst[k], a.n[k], tile, factor, norm); break;
+        default: tile_scale(a, (const f16_t *)a.src[k], (f16_t *)a.dst[k], a.n[k], tile, factor, norm); break;
         }
     }
 }

@@ -131,3 +131,28 @@ def test_a_double_norm_past_its_range_changes_nothing(la):
     x = make(1000, 1.7e308, F64)
     y = x.clone()
     assert float(la.clip_gradients([x], 1.0)) == math.inf and same(x, y)
+
+
+@pytest.mark.parametrize("dtype,size,limit", [(F32, 1e37, 1e-5), (F32, 1e37, 1e-2), (BF16, 1e37, 1e-5), (F32, 1e37, 1e-20), (F64, 1e306, 1e-3), (F64, 1e300, 1e-250)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_factors_below_the_smallest_normal_number(la, dtype, size, limit, shift):
+    """the factor is rounded as a number of its type only where that costs nothing"""
+    grads = [make(700, size, dtype), make(33, size, dtype, seed=2)]
+    norm = value(norm_of(grads))
+    assert limit / norm < (2.0 ** -1022 if dtype == F64 else 2.0 ** -126)
+    want = [x.double() * 1e-200 * (limit / (norm * 1e-200)) for x in grads]
+    space = [torch.empty(x.numel() + 1, dtype=dtype, device="cuda") for x in grads]
+    out = [s[shift:shift + x.numel()] for s, x in zip(space, grads)]
+    la.clip_gradients(grads, limit, out=out)
+    for x, y in zip(out, want):
+        assert f.rel(x, y) <= f.tolerance(dtype)
+    mine = [x.clone() for x in grads]
+    la.clip_gradients(mine, limit)
+    for x, y in zip(mine, want):
+        assert f.rel(x, y) <= f.tolerance(dtype)
+
+
+def test_a_limit_of_zero_clears_the_largest_numbers(la):
+    for x in (make(100, 1e37, F32), make(100, 1e300, F64), make(100, 1e37, BF16)):
+        la.clip_gradients([x], 0.0)
+        assert not x.any()
