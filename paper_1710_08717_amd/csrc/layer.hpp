@@ -9,6 +9,8 @@ namespace la {
 inline bool unknown_dtype(la_dtype dt) { return dt != LA_F32 && dt != LA_F64 && dt != LA_BF16 && dt != LA_F16; }
 inline bool small_dtype(la_dtype dt) { return dt == LA_BF16 || dt == LA_F16; }
 inline size_t bytes_of(la_dtype dt) { return dt == LA_F64 ? 8 : dt == LA_F32 ? 4 : 2; }
+// the most blocks of `threads` that one launch takes: its threads are counted in 32 bits
+inline int64_t most_blocks(int threads) { return (int64_t)(0xffffffffu / (unsigned)threads); }
 inline size_t align_up(size_t n) { return (n + 255) & ~(size_t)255; }
 inline bool overlaps(const void *a, size_t na, const void *b, size_t nb)
 {

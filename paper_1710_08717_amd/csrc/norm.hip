@@ -381,6 +381,23 @@ static int norm_blocks(int64_t rows, NormShape s)
     return (int)(s.tpr == 0 ? (rows < 64 ? rows : 64) : all < most ? all : most);
 }
 
+// A launch has fewer than 2^32 threads: more rows than those serve are taken in pieces, launch(args, blocks) for each.
+template <typename T, class F>
+static void by_rows(NormArgs p, int rows_of_block, int threads, F &&launch)
+{
+    const int64_t all = p.rows, most = most_blocks(threads) * rows_of_block;
+    const size_t stat = sizeof(acc_of<T>);
+    for (int64_t at = 0; at < all; at += most) {
+        p.rows = all - at < most ? all - at : most;
+        launch(p, (unsigned)((p.rows + rows_of_block - 1) / rows_of_block));
+        p.x = (const T *)p.x + most * p.ldx;
+        p.y = (T *)p.y + most * p.n;
+        p.yb = p.yb ? (const T *)p.yb + most * p.n : nullptr;
+        p.mean = p.mean ? (char *)p.mean + most * stat : nullptr;
+        p.rstd = p.rstd ? (char *)p.rstd + most * stat : nullptr;
+    }
+}
+
 template <typename T, int TPR, int R>
 static void norm_launch(const NormArgs &p, bool back, hipStream_t st)
 {
@@ -392,7 +409,7 @@ static void norm_launch(const NormArgs &p, bool back, hipStream_t st)
             LA_LAUNCH((k_layer_norm_back<T, TPR, R>), dim3(norm_blocks(p.rows, {TPR, R})), dim3(NT), 0, st, p);
     if constexpr (FORWARD)
         if (!back)
-            LA_LAUNCH((k_layer_norm<T, TPR, R>), dim3((unsigned)((p.rows + GROUPS - 1) / GROUPS)), dim3(NT), 0, st, p);
+            by_rows<T>(p, GROUPS, NT, [&](const NormArgs &q, unsigned blocks) { LA_LAUNCH((k_layer_norm<T, TPR, R>), dim3(blocks), dim3(NT), 0, st, q); });
 }
 
 template <typename T>
@@ -425,11 +442,11 @@ static la_status norm_t(const NormArgs &p, bool back, void *wb, void *cb, int wt
     if (s.tpr) {
         norm_dispatch<T>(p, s, back, st);
     } else if (!back) {
-        LA_LAUNCH((k_layer_norm_wide<T>), dim3((unsigned)p.rows), dim3(1024), 0, st, p);
+        by_rows<T>(p, 1, 1024, [&](const NormArgs &q, unsigned blocks) { LA_LAUNCH((k_layer_norm_wide<T>), dim3(blocks), dim3(1024), 0, st, q); });
     } else {
         if (wb || cb)  // (first: x_bar may be written over y_bar)
             LA_LAUNCH((k_norm_columns_wide<T>), dim3((p.n + 255) / 256, parts), dim3(256), 0, st, p);
-        LA_LAUNCH((k_layer_norm_back_wide<T>), dim3((unsigned)p.rows), dim3(1024), 0, st, p);
+        by_rows<T>(p, 1, 1024, [&](const NormArgs &q, unsigned blocks) { LA_LAUNCH((k_layer_norm_back_wide<T>), dim3(blocks), dim3(1024), 0, st, q); });
     }
     if (back && (wb || cb))
         LA_LAUNCH((k_norm_parts<A>), dim3((p.n + 31) / 32, 2), dim3(1024), 0, st, (const A *)p.part, parts, p.n, wb, cb, wtype);
@@ -446,7 +463,7 @@ static la_status norm_any(la_dtype dt, const NormArgs &p, bool back, void *wb, v
     }
 }
 
-constexpr int64_t NORM_MAX_ROWS = 0x7fffffff;  // (a block or part of one a row)
+constexpr int64_t NORM_MAX_ROWS = 0x7fffffff;
 constexpr int NORM_MAX_N = 1 << 26;            // (columns and the strides over them are int)
 
 static bool norm_sizes_bad(la_dtype dt, la_dtype wdt, int64_t rows, int n, int64_t ldx)
