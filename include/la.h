@@ -340,7 +340,7 @@ la_status la_kalman_filter(la_dtype dt, int64_t batch, int T, int dh, int dv, in
  *   o_t = scale S_t^T q_t.
  * dt is LA_F32, LA_BF16 or LA_F16 (LA_F64: LA_ERR_UNSUPPORTED), the type of q, k, v, o and their gradients;
  * g, beta, the states and their gradients are float.  1 <= dk <= 128, 1 <= dv <= 1024, hv dv and
- * ldv at most 2^24 (above: LA_ERR_UNSUPPORTED).
+ * ldv at most 2^24, batch hv ceil(dv / 64) below 2^23 (above: LA_ERR_UNSUPPORTED).
  * Value head h reads key head h / (hv / hk); hk divides hv.
  *   q, k [tokens of all sequences, hk, dk], v [.., hv, dv]: ldq, ldk, ldv elements from a token to the
  *   next (views of a wider projection); g, beta [.., hv], o [.., hv, dv] dense.
@@ -377,7 +377,8 @@ la_status la_delta_rule_backward(la_dtype dt, int64_t batch, int64_t tokens, int
 /* One token of each of `batch` sequences, for serving: q, k [batch, hk, dk], v [batch, hv, dv] (ldq, ldk, ldv elements
  * from a sequence to the next), g, beta [batch, hv], o [batch, hv, dv].  state [slots, hv, dk, dv]: a cache of states, updated
  * in place; sequence n has state slot[n] (int32, device), or n where slot is NULL.  A slot outside 0 .. slots - 1 has no state:
- * o is zero and nothing is updated.  The slots of one call are distinct.  No scratch memory. */
+ * o is zero and nothing is updated.  The slots of one call are distinct.  batch hv ceil(dv / 32) is below 2^24 (else LA_ERR_UNSUPPORTED).
+ * No scratch memory. */
 la_status la_delta_rule_step(la_dtype dt, int64_t batch, int hk, int hv, int dk, int dv, const void *q, int64_t ldq, const void *k,
                              int64_t ldk, const void *v, int64_t ldv, const float *g, const float *beta, double scale,
                              float *state, int64_t slots, const int32_t *slot, void *o, void *stream);

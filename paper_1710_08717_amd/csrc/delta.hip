@@ -627,11 +627,15 @@ static void walk(DeltaArgs &p, hipStream_t st)
 template <typename T, int DKP, bool SAVE>
 static la_status scan_s(DeltaArgs &p, hipStream_t st)
 {
+    using G = Pack<T, DKP>;
     p.pack_heads = p.slots * p.hv <= 2 * COMPUTE_UNITS ? 1 : p.hv / p.hk;
+    const int groups = G::PAIRED || walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2 ? 2 : 4;
+    // (segments are for few heads: their launches are small)
+    if (p.slots * (p.hv / p.pack_heads) > most_blocks(256) || p.batch * p.hv * ((p.dv + 16 * groups - 1) / (16 * groups)) > most_blocks(128 * groups))
+        return LA_ERR_UNSUPPORTED;
     if (p.slots > 0)
         LA_LAUNCH((k_delta_pack<T, DKP, SAVE>), dim3((unsigned)(p.slots * (p.hv / p.pack_heads))), dim3(256), 0, st, p);
-    using G = Pack<T, DKP>;
-    if (G::PAIRED || walk_groups((p.seg ? p.segs : p.batch) * p.hv, p.dv) == 2)
+    if (groups == 2)
         walk<T, DKP, 2, SAVE>(p, st);
     else if constexpr (!G::PAIRED)
         walk<T, DKP, 4, SAVE>(p, st);
@@ -980,7 +984,7 @@ la_status la_delta_rule_step(la_dtype dt, int64_t batch, int hk, int hv, int dk,
         return LA_OK;
     if (!q || !k || !v || !g || !beta || !o || (slots > 0 && !state) || (!slot && batch > slots))
         return LA_ERR_INVALID_ARG;
-    if (batch > 0x7fffffff / hv / ((dv + 31) / 32))
+    if (batch > most_blocks(256) / hv / ((dv + 31) / 32))
         return LA_ERR_UNSUPPORTED;
     const size_t es = bytes_of(dt), ob = (size_t)batch * hv * dv * es, sb = (size_t)slots * hv * dk * dv * 4, gb = (size_t)batch * hv * 4;
     const size_t qs = ((size_t)(batch - 1) * ldq + (size_t)hk * dk) * es, ks = ((size_t)(batch - 1) * ldk + (size_t)hk * dk) * es,

@@ -604,13 +604,15 @@ __global__ __launch_bounds__(4 * DKP) void k_delta_grads(DeltaArgs p)
 template <typename T, int DKP>
 static la_status back_t(DeltaArgs &p, hipStream_t st)
 {
-    if (walk_groups(p.batch * p.hv, p.dv) == 2) {
-        p.slices = (p.dv + 31) / 32;
-        LA_LAUNCH((k_delta_scan_back<T, DKP, 2>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(256), 0, st, p);
-    } else {
-        p.slices = (p.dv + 63) / 64;
-        LA_LAUNCH((k_delta_scan_back<T, DKP, 4>), dim3((unsigned)(p.batch * p.hv * p.slices)), dim3(512), 0, st, p);
-    }
+    const int groups = walk_groups(p.batch * p.hv, p.dv);
+    p.slices = (p.dv + 16 * groups - 1) / (16 * groups);
+    const int64_t blocks = p.batch * p.hv * p.slices;
+    if (blocks > most_blocks(128 * groups) || p.slots * p.hk > most_blocks(4 * DKP))
+        return LA_ERR_UNSUPPORTED;
+    if (groups == 2)
+        LA_LAUNCH((k_delta_scan_back<T, DKP, 2>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+    else
+        LA_LAUNCH((k_delta_scan_back<T, DKP, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p);
     if (p.slots > 0)
         LA_LAUNCH((k_delta_grads<T, DKP>), dim3((unsigned)(p.slots * p.hk)), dim3(4 * DKP), 0, st, p);
     return launch_check("delta rule backward");
