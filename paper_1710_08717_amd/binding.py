@@ -559,6 +559,13 @@ def _shape(name, t, want):
         raise LaError(f"{name}: shape {tuple(want)} is wanted, got {tuple(t.shape)}")
 
 
+def _sizes_fit(**sizes):
+    """ctypes takes an int modulo 2^32: what the C entries' own ints do not hold ends here."""
+    for name, n in sizes.items():
+        if n > 0x7FFFFFFF:
+            raise LaError(f"{name}: sizes of up to 2^31 - 1 are taken, got {n} (LA_ERR_UNSUPPORTED)")
+
+
 def _rows(name, t, inner):
     """Elements from one row to the next of a tensor whose last `inner` axes are dense and whose leading axes are rows one distance apart."""
     want = 1
@@ -611,6 +618,7 @@ class _Delta:
             if t.dtype != q.dtype or t.device != q.device:
                 raise LaError("q, k and v must share dtype and device")
         self.hk, self.dk, self.hv, self.dv = q.shape[-2], q.shape[-1], v.shape[-2], v.shape[-1]
+        _sizes_fit(hk=self.hk, dk=self.dk, hv=self.hv, dv=self.dv)
         self.lead = tuple(q.shape[:lead])
         _shape("k", k, q.shape)
         if tuple(v.shape[:lead]) != self.lead:
@@ -718,6 +726,7 @@ def _norm_input(x):
         raise LaError("tensors must be on the GPU")
     if x.dim() < 1:
         raise LaError("x: at least one axis is wanted")
+    _sizes_fit(x=x.shape[-1])
     return _layer_dt(x), _batch(x, 1), x.shape[-1], _rows("x", x, 1)
 
 
