@@ -699,7 +699,7 @@ def delta_rule_step(q, k, v, g, beta, state, slots=None, scale=None, out=None):
     o = torch.empty(v.shape, dtype=v.dtype, device=v.device) if out is None else out
     _shape("out", o, v.shape)
     _on_gpu(v.device, v.dtype, out=o)
-    _shape("state", state, (state.shape[0], d.hv, d.dk, d.dv))
+    _shape("state", state, (*state.shape[:1], d.hv, d.dk, d.dv))
     _on_gpu(v.device, torch.float32, state=state)
     _on_gpu(v.device, torch.int32, slots=slots)
     _shape("slots", slots, (d.batch,))

@@ -1,4 +1,4 @@
-"""Sizes past the C entries' integers are refused by the binding, in both its ways, and not taken modulo 2^32."""
+"""Sizes past the C entries' integers are refused by the binding, in both its ways, and not taken modulo 2^32; states of the wrong number of axes as well."""
 import sys
 
 import pytest
@@ -53,3 +53,10 @@ def test_heads_of_the_delta_rule(la, which):
                  lambda: la.delta_rule_step(q, q, v, g, g, state, slots=torch.zeros(1, dtype=torch.int32, device="cuda"))):
         with pytest.raises(la.LaError):
             call()
+
+
+@pytest.mark.parametrize("shape", [(), (3,), (3, 2, 4), (3, 2, 4, 5, 1), (3, 2, 5, 4)])
+def test_states_of_the_wrong_shape(la, shape):
+    q, v, g = torch.zeros(3, 1, 4, device="cuda"), torch.zeros(3, 2, 5, device="cuda"), torch.zeros(3, 2, device="cuda")
+    with pytest.raises(la.LaError):
+        la.delta_rule_step(q, q, v, g, g, torch.zeros(shape, device="cuda"))
