@@ -591,6 +591,11 @@ def _rows(name, t, inner):
     return want if ld is None else ld
 
 
+def _written(*tensors):
+    """Tensors of the caller's that a call has written: autograd is told, as of torch's own operators in place."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _scratch(workspace, need, t):
     """(tensor, pointer, bytes): the caller's uint8 device tensor, or a fresh one where the call needs some and none was given."""
     if workspace is not None:
@@ -662,6 +667,7 @@ def delta_rule(q, k, v, g, beta, scale=None, initial_state=None, offsets=None, w
         buf, wp, wb = (None, 0, 0) if keep else _scratch(workspace, int(lib.la_delta_rule_workspace_bytes(*d.sizes, packed)), q)
         _check(lib.la_delta_rule(*d.sizes, _ptr(offsets), *d.inputs, d.scale(scale), _ptr(initial_state), _ptr(o), _ptr(state), _ptr(saved),
                                  saved.numel() if keep else 0, wp, wb, _stream(q)), "la_delta_rule")
+    _written(out)
     return o, state, saved
 
 
@@ -706,6 +712,7 @@ def delta_rule_step(q, k, v, g, beta, state, slots=None, scale=None, out=None):
     with _on_device(q):
         _check(load().la_delta_rule_step(d.dt, d.batch, d.hk, d.hv, d.dk, d.dv, *d.inputs, d.scale(scale), _ptr(state), state.shape[0], _ptr(slots),
                                          _ptr(o), _stream(q)), "la_delta_rule_step")
+    _written(state, out)
     return o
 
 
@@ -747,6 +754,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, out=None):
     with _on_device(x):
         _check(load().la_layer_norm(dt, _LAYER_TYPES[wdt], rows, n, ld, _ptr(x), _ptr(weight), _ptr(bias), float(eps), _ptr(y), _ptr(mean), _ptr(rstd),
                                     _stream(x)), "la_layer_norm")
+    _written(out)
     return y, mean, rstd
 
 
@@ -773,6 +781,7 @@ def layer_norm_backward(x, y_bar, mean, rstd, weight=None, want_weights=True, ou
         buf, wp, wbytes = _scratch(workspace, int(lib.la_layer_norm_backward_workspace_bytes(dt, rows, n)), x)
         _check(lib.la_layer_norm_backward(dt, _LAYER_TYPES[wdt], rows, n, ld, _ptr(x), _ptr(y_bar), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(x_bar),
                                           _ptr(wb), _ptr(bb), wp, wbytes, _stream(x)), "la_layer_norm_backward")
+    _written(out)
     return x_bar, wb, bb
 
 
@@ -812,4 +821,5 @@ def clip_gradients(grads, max_norm, out=None, workspace=None):
         buf, wp, wb = _scratch(workspace, int(lib.la_clip_gradients_workspace_bytes(count, sizes)), first)
         _check(lib.la_clip_gradients(count, types, sizes, src, dst, float(max_norm), int(wide), _ptr(norm), wp, wb, _stream(first)),
                "la_clip_gradients")
+    _written(*outs)
     return norm

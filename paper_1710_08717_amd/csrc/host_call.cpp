@@ -553,6 +553,13 @@ struct LayerCall : Call {
     }
 };
 
+// A tensor of the caller's that a call has written: autograd is told, as of torch's own operators in place.  (An inference tensor has no versions.)
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference())
+        t.unsafeGetTensorImpl()->bump_version();
+}
+
 // [batch, heads, size] whose heads and elements are dense: elements from one sequence to the next, or -1
 int64_t step_rows(const at::Tensor &t)
 {
@@ -597,7 +604,10 @@ LA_FUNCTION(delta_rule_step, 8)
                                    (const float *)g->data_ptr(), (const float *)beta->data_ptr(), scale, (float *)state->data_ptr(), state->size(0),
                                    slots ? (const int32_t *)slots->data_ptr() : nullptr, o.data_ptr(), st);
     });
-    return s == LA_OK ? wrap(o) : nullptr;
+    if (s != LA_OK)
+        return nullptr;
+    written(*state);
+    return wrap(o);
 }
 
 // the type of weight and bias beside x: x's own, or float32 beside 16 bits
@@ -721,7 +731,11 @@ LA_FUNCTION(clip_gradients, 3)
         c.scratch(lib.clip_gradients_workspace_bytes((int)n, sizes.data()));
         return lib.clip_gradients((int)n, types.data(), sizes.data(), src.data(), dst.data(), limit, wide ? LA_F64 : LA_F32, norm.data_ptr(), c.wp, c.wb, st);
     });
-    return s == LA_OK ? wrap(norm) : nullptr;
+    if (s != LA_OK)
+        return nullptr;
+    for (size_t i = 1; i < held.size(); i += 2)  // (the outputs)
+        written(held[i]);
+    return wrap(norm);
 }
 
 // bind(path): the library whose functions are called
