@@ -160,7 +160,7 @@ __device__ __forceinline__ void tile_scale(const ClipArgs &a, const T *p, T *q, 
             q[i] = (T)(A)((double)(A)p[i] * 0x1p-100 * g);
         return;
     }
-    if (((uintptr_t)p & 15) != ((uintptr_t)q & 15)) {  // no pack starts on 16 bytes in both
+    if (((uintptr_t)p & 15) != ((uintptr_t)q & 15)) {  // no pack starts on 16 bytes in both: by elements (200 million of bf16: 509 us for both passes, else 225)
         for (int64_t i = at + threadIdx.x; i < to; i += 256)
             q[i] = (T)((A)p[i] * f);
         return;

@@ -661,8 +661,8 @@ la_status launch_delta_rule(la_dtype dt, DeltaArgs p, bool save, hipStream_t st)
 // one token of every sequence
 // ---------------------------------------------------------------------------------
 // With s = S^T k and y = S^T q from one read of the state, the new state is a S + k u^T and the answer scale (a y + (q.k) u): the state is read and written
-// once, which is what bounds the call (128 sequences, 32 heads of 128 x 128, bf16: 540 MB in 106 us, 5.1 TB/s, what a copy reaches; one sequence: 4.5 us, a
-// launch and one round trip).  A block takes 32 columns of one state, its lanes packs of VEC columns by rows; all loads of a lane are in
+// once, which is what bounds the call (128 sequences, 32 heads of 128 x 128, bf16: 540 MB, 96 us for the kernel by itself, 115 us a call among others, 4.7 TB/s
+// where a copy reaches 5.1; one sequence: 4.5 us, a launch and one round trip).  A block takes 32 columns of one state, its lanes packs of VEC columns by rows; all loads of a lane are in
 // flight at once.
 struct DeltaStepArgs {
     const void *q, *k, *v;
@@ -822,7 +822,9 @@ static la_status delta_sizes(la_dtype dt, int64_t batch, int64_t tokens, int hk,
     const size_t heads = (size_t)z.slots * hv;
     // Segments where whole sequences would leave three quarters of the compute units idle, as many as fill them, of 8 chunks at least and up to 8 of a
     // sequence of the average length: a sequence of g segments takes the time of about 2 / g of it (heads of 128, bf16, in us with and without: 8192 tokens,
-    // 16 heads 250 and 540, 32 heads 530 and 583, 40 heads, which make three segments, 685 and 620; 16 heads, 24 chunks 81 and 99, 16 chunks 71 and 66).
+    // 16 heads 250 and 540, 32 heads 530 and 583, 40 heads, which make three segments, 685 and 620; 16 heads, 24 chunks 81 and 99, 16 chunks 71 and 66; of 128
+    // chunks of f16 and f32, 16 heads 208 and 347, 244 and 419, 32 heads 376 and 420, 469 and 514; of 24 chunks, 16 heads 70 and 76, 73 and 82; 32 heads of 32
+    // chunks are the exception, bf16 140 and 133, f16 116 and 106, f32 125 and 116).  A long sequence among short ones, whose average is below 24, is walked whole.
     const int64_t blocks = batch * hv * ((dv + 63) / 64);
     if (blocks > 0 && blocks * 4 <= COMPUTE_UNITS) {
         const int64_t each = (z.all / batch + z.c - 1) / z.c, most_parts = COMPUTE_UNITS / blocks < 8 ? COMPUTE_UNITS / blocks : 8;
